@@ -87,7 +87,7 @@ def draw(rng):
     if kind == "append":
         src, dst = rng.choice([("bf16", "bf16"), ("f32", "bf16"), ("f32", "f32")])
         batch = _log_int(rng, 1, 64)
-        q_hi = _log_int(rng, 1, max(1, min(1024, 8192 // batch)))
+        q_hi = _log_int(rng, 1, max(1, min(1024, (8192 if src == "bf16" else 4096) // batch)))
         q_lo = rng.randint(max(0, q_hi // 2), q_hi)
         past = _log_int(rng, 1, 2048)
         return dict(_append("", batch, q_lo, q_hi, q_hi + past // 2, q_hi + past, heads, page, src, dst))
