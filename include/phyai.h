@@ -499,6 +499,106 @@ phyai_status_t phyai_batcher_next(phyai_batcher_t *b, double timeout_ms, uint64_
 uint32_t phyai_batcher_pending(phyai_batcher_t *b);
 phyai_status_t phyai_batcher_plan(const phyai_batcher_config_t *cfg, uint32_t n, int32_t *slots, uint32_t *active_workers);
 
+/*
+ * Paged cache of keys and values, for the backbone that fills a prefix: chunks of new tokens are appended to pages and attend over
+ * them (Sec. "Architecture": the model runner owns the caches; results section: the prefix is prefilled once and then frozen for the
+ * Euler steps), and the finished prefix is packed into the ragged cache that phyai_denoise_batched reads.
+ *
+ *   pages       device, [n_layers][2 (K,V)][n_pages * page_size][n_kv_heads][head_dim], head_dim contiguous, 16-byte aligned: the layout of
+ *               the prefix cache, one page number for all layers and both planes
+ *   head_dim    64, 128 or 256;  page_size  16, 32, 64, 128 or 256;  dtype  PHYAI_F32 or PHYAI_BF16
+ * Requests of a call:
+ *   cu_q_lens   device int32 [batch + 1], non-decreasing, cu[0] >= 0, cu[batch] <= tokens: request b's new tokens are token rows
+ *               cu[b] .. cu[b + 1] - 1; token rows of no request are neither read nor written
+ *   kv_lens     device int32 [batch]: cached tokens of request b WITH its new ones, which are the last; <= max_pages * page_size
+ *   page_table  device int32 [batch][max_pages]: cached token t of request b is row page_table[b][t / page_size] * page_size +
+ *               t % page_size of the planes; entries past a request's last page are not read
+ *   batch <= 1024.  Requests may share pages that they only read; a page that two requests of an append write holds the tokens of
+ *   either.
+ *   status_word device int32, zeroed by the caller; a violation found on the device sets it to PHYAI_ERR_INVALID_ARG.  Lengths out of
+ *               order: the call writes nothing.  A table entry that names no page, a position outside the rotary table: nothing outside the
+ *               buffers is read or written, what the call writes for the tokens or requests concerned is not specified.  A call that finds the
+ *               word raised writes nothing.  (PHYAI_ERR_TIMEOUT: a bounded wait inside a kernel expired.)
+ * The calls only enqueue work on `stream` (of the current device) and allocate nothing.  Errors: INVALID_ARG, UNSUPPORTED, CUDA; message in
+ * phyai_paged_last_error().
+ */
+typedef struct {
+  uint32_t struct_size;
+  uint32_t n_layers, n_kv_heads, head_dim, page_size;
+  uint32_t dtype;   /* phyai_dtype_t */
+  uint64_t n_pages;
+  void *pages;
+} phyai_paged_cache_t;
+
+/* Heads of a call's rows; types: BF16 -> BF16, F32 -> BF16, F32 -> F32. */
+typedef struct {
+  uint32_t struct_size;
+  uint32_t n_q_heads, n_kv_heads, head_dim;
+  uint32_t in_dtype, out_dtype;   /* phyai_dtype_t */
+  float eps;                      /* of the norm, inside the square root */
+} phyai_heads_desc_t;
+
+/*
+ * Norm of every query and key head with the position rotation in the same pass (K as phyai_pack_prefix_kv and the prefix cache want
+ * it): y = x / sqrt(mean(x^2) + eps) * (1 + gain), then (y_j, y_{j + dh/2}) rotated by the angle of the token's position.
+ *   q, k        device, `tokens` rows of n_q_heads / n_kv_heads heads of head_dim, heads contiguous in a row, rows q_stride / k_stride
+ *               elements apart (columns of a fused q|k|v matrix); q may be NULL: k only
+ *   positions   device int32 [tokens], 0 <= position < n_positions (NULL without a table)
+ *   rope_cos_sin  device float32 [n_positions][head_dim/2][2] as phyai_suffix_attention takes it, or NULL: no rotation
+ *   q_gain, k_gain  device float32 [head_dim], or NULL: no norm of those heads
+ *   q_out, k_out  device, contiguous rows [tokens][heads][head_dim]; may be q / k themselves where type and stride are the same, and
+ *               otherwise overlap no input
+ * fp32 arithmetic, one rounding.  Pointers and strides: multiples of 16 bytes.
+ */
+phyai_status_t phyai_norm_rope_heads(const phyai_heads_desc_t *desc, uint32_t tokens, const void *q, uint64_t q_stride, const void *k,
+                                     uint64_t k_stride, const int32_t *positions, const float *rope_cos_sin, uint64_t n_positions,
+                                     const float *q_gain, const float *k_gain, void *q_out, void *k_out, int32_t *status_word, void *stream);
+
+/*
+ * Append: K (normed and rotated as above) and V of the new tokens go to their places in the pages of `layer`; with q, its normed and
+ * rotated rows go to q_out in the same pass.  kv_lens counts the new tokens already: cu[b + 1] - cu[b] <= kv_lens[b].
+ *   positions   device int32 [tokens] for the rotation, or NULL: the token's place in its cache
+ *   desc        n_kv_heads, head_dim, out_dtype as the cache's
+ */
+phyai_status_t phyai_append_paged_kv(const phyai_paged_cache_t *cache, const phyai_heads_desc_t *desc, uint32_t layer, uint32_t tokens,
+                                     const void *q, uint64_t q_stride, const void *k, uint64_t k_stride, const void *v, uint64_t v_stride,
+                                     uint32_t batch, const int32_t *cu_q_lens, const int32_t *kv_lens, const int32_t *page_table,
+                                     uint32_t max_pages, const int32_t *positions, const float *rope_cos_sin, uint64_t n_positions,
+                                     const float *q_gain, const float *k_gain, void *q_out, int32_t *status_word, void *stream);
+
+/*
+ * Attention of the new tokens over the pages of `layer` (their own keys and values have been appended).  Row i of request b, at place
+ * p = kv_lens[b] - (cu[b + 1] - cu[b]) + i of its cache, sees keys [0, limit):
+ *   causal 0    limit = kv_lens[b]
+ *   causal 1    limit = max(p + 1, prefix_lens[b]), at most kv_lens[b]; prefix_lens: device int32 [batch] or NULL (0): image and prompt
+ *               tokens that see one another
+ * A row that sees no key is zero; keys that a row does not see have no part in it, whatever they hold.
+ *   q           device, token rows of n_q_heads heads (a multiple of n_kv_heads; head h reads kv head h / (n_q_heads / n_kv_heads)), of the
+ *               cache's type, q_stride elements apart, already rotated
+ *   scale       of the logits; 0 = 1 / sqrt(head_dim)
+ *   out         device, [tokens][n_q_heads][head_dim], the cache's type; overlaps no input
+ *   workspace   device, 16-byte aligned, phyai_paged_attention_workspace_bytes() bytes with the same sizes (on the same kind of device): this call's
+ *               until its work has run.  Calls that may overlap (other streams, captured graphs replayed side by side) need one each
+ */
+size_t phyai_paged_attention_workspace_bytes(const phyai_paged_cache_t *cache, uint32_t n_q_heads, uint32_t tokens, uint32_t batch,
+                                             uint32_t max_pages);
+phyai_status_t phyai_paged_attention(const phyai_paged_cache_t *cache, uint32_t layer, uint32_t n_q_heads, uint32_t tokens, const void *q,
+                                     uint64_t q_stride, uint32_t batch, const int32_t *cu_q_lens, const int32_t *kv_lens,
+                                     const int32_t *page_table, uint32_t max_pages, uint32_t causal, const int32_t *prefix_lens, float scale,
+                                     void *out, void *workspace, size_t workspace_bytes, int32_t *status_word, void *stream);
+
+/*
+ * Pages -> the ragged prefix cache: cached tokens 0 .. kv_lens[b] - 1 of request b, of every layer, go to rows cu[b] .. of prefix_kv
+ * [n_layers][2][kv_tokens][n_kv_heads][head_dim]; cu_prefix_lens (device int32 [batch + 1], written) is the exclusive prefix sum of kv_lens.
+ * Rows >= cu[batch] are left untouched.  sum(kv_lens) > kv_tokens: the status word is raised, nothing is copied.  Bit-exact copy.
+ */
+phyai_status_t phyai_pack_paged_kv(const phyai_paged_cache_t *cache, uint32_t batch, const int32_t *kv_lens, const int32_t *page_table,
+                                   uint32_t max_pages, void *prefix_kv, uint64_t kv_tokens, int32_t *cu_prefix_lens, int32_t *status_word,
+                                   void *stream);
+
+/* Thread-local description of the last error of an entry point of the paged cache. */
+const char *phyai_paged_last_error(void);
+
 /* Thread-local description of the last error of an operator entry point. */
 const char *phyai_op_last_error(void);
 

@@ -32,7 +32,8 @@ EXPORTS = ("phyai_expert_create", "phyai_expert_destroy", "phyai_prefix_kv_bytes
            "phyai_pack_prefix_kv", "phyai_pack_prefix_kv_cleared", "phyai_postprocess_actions", "phyai_adapter_last_error", "phyai_batcher_create",
            "phyai_batcher_destroy", "phyai_batcher_submit", "phyai_batcher_next", "phyai_batcher_pending",
            "phyai_batcher_plan", "phyai_w8a8_project", "phyai_w8a8_last_error", "phyai_project_features_kv", "phyai_kv_projector_create",
-           "phyai_kv_projector_run", "phyai_kv_projector_destroy")
+           "phyai_kv_projector_run", "phyai_kv_projector_destroy", "phyai_norm_rope_heads", "phyai_append_paged_kv", "phyai_paged_attention",
+           "phyai_paged_attention_workspace_bytes", "phyai_pack_paged_kv", "phyai_paged_last_error")
 
 
 class PhyaiError(RuntimeError):
@@ -64,6 +65,15 @@ class KvPackDesc(C.Structure):
 
 
 _KV_PACK_SIZE = C.sizeof(KvPackDesc)
+
+
+class PagedCacheDesc(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "n_layers", "n_kv_heads", "head_dim", "page_size", "dtype")] + \
+               [("n_pages", C.c_uint64), ("pages", C.c_void_p)]
+
+
+class HeadsDesc(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "n_q_heads", "n_kv_heads", "head_dim", "in_dtype", "out_dtype")] + [("eps", C.c_float)]
 
 
 class BatcherConfig(C.Structure):
@@ -139,6 +149,15 @@ def load_library() -> C.CDLL:
     lib.phyai_batcher_pending.argtypes = [_VP]
     lib.phyai_batcher_pending.restype = C.c_uint32
     lib.phyai_batcher_plan.argtypes = [C.POINTER(BatcherConfig), C.c_uint32, C.POINTER(C.c_int32), C.POINTER(C.c_uint32)]
+    u32, u64 = C.c_uint32, C.c_uint64
+    lib.phyai_norm_rope_heads.argtypes = [_VP, u32, _VP, u64, _VP, u64, _VP, _VP, u64, _VP, _VP, _VP, _VP, _VP, _VP]
+    lib.phyai_append_paged_kv.argtypes = [_VP, _VP, u32, u32, _VP, u64, _VP, u64, _VP, u64, u32, _VP, _VP, _VP, u32, _VP, _VP, u64, _VP, _VP,
+                                          _VP, _VP, _VP]
+    lib.phyai_paged_attention.argtypes = [_VP, u32, u32, u32, _VP, u64, u32, _VP, _VP, _VP, u32, u32, _VP, C.c_float, _VP, _VP, C.c_size_t, _VP, _VP]
+    lib.phyai_paged_attention_workspace_bytes.argtypes = [_VP, u32, u32, u32, u32]
+    lib.phyai_paged_attention_workspace_bytes.restype = C.c_size_t
+    lib.phyai_pack_paged_kv.argtypes = [_VP, u32, _VP, _VP, u32, _VP, u64, _VP, _VP, _VP]
+    lib.phyai_paged_last_error.restype = C.c_char_p
     _lib = lib
     return lib
 
@@ -482,6 +501,195 @@ def w8a8_project(x: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
     if st != OK:
         raise PhyaiError(st, lib.phyai_w8a8_last_error().decode())
     return (y, codes, scales) if return_codes else y
+
+
+_STORE = {torch.float32: DTYPES["f32"], torch.bfloat16: DTYPES["bf16"]}
+
+
+class _Launch:
+    """Device and stream of a call: the tensors' device becomes the current one, outputs are allocated on the call's stream."""
+
+    def __init__(self, device: torch.device, stream):
+        self.device = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+        self.stream = None if stream is None else torch.cuda.stream(stream)
+        self.raw = _raw_stream(stream, device) or None
+
+    def __enter__(self):
+        if self.device is not None:
+            self.device.__enter__()
+        if self.stream is not None:
+            self.stream.__enter__()
+        return self.raw
+
+    def __exit__(self, *exc):
+        if self.stream is not None:
+            self.stream.__exit__(*exc)
+        if self.device is not None:
+            self.device.__exit__(*exc)
+
+
+def _head_rows(name: str, t: torch.Tensor, device: torch.device, like: Optional[torch.Tensor] = None) -> int:
+    """Checks rows of heads ``[T, heads, dh]`` (heads contiguous in a row); returns the row stride in elements."""
+    if t.dim() != 3 or t.dtype not in _STORE or t.device != device:
+        raise ValueError(f"{name} must be a float32 or bfloat16 tensor [tokens, heads, head_dim] on {device}")
+    T, H, dh = t.shape
+    row, head, one = t.stride()
+    if (dh > 1 and one != 1) or (H > 1 and head != dh):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    if like is not None and (T != like.shape[0] or dh != like.shape[2] or t.dtype != like.dtype):
+        raise ValueError(f"{name} and the keys differ in tokens, head_dim or type")
+    return row if T > 1 else H * dh
+
+
+def _ints(name: str, t: torch.Tensor, device: torch.device, *shape) -> int:
+    if t.dtype != torch.int32 or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _floats(name: str, t: Optional[torch.Tensor], device: torch.device, *shape) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.device != device or t.shape[-len(shape):] != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor {list(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _paged_check(lib, st: int):
+    if st != OK:
+        raise PhyaiError(st, lib.phyai_paged_last_error().decode())
+
+
+def norm_rope_heads(q: Optional[torch.Tensor], k: torch.Tensor, positions: Optional[torch.Tensor], rope_cos_sin: Optional[torch.Tensor],
+                    q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None, stream=None):
+    """Norm (gain ``1 + gain``; None: no norm) of every head of ``q`` ``[T, Hq, dh]`` and ``k`` ``[T, Hkv, dh]`` with the rotation by
+    ``positions`` (int32 ``[T]``) in the same pass; rows may be columns of a fused matrix.  Returns (q, k) in ``dtype`` (default: as
+    given).  ``status``: int32 word that a position outside the table raises (zeroed by the caller; None: a fresh one, not returned)."""
+    lib = _lib or load_library()
+    device = k.device
+    k_row = _head_rows("k", k, device)
+    q_row = 0 if q is None else _head_rows("q", q, device, k)
+    T, Hkv, dh = k.shape
+    Hq = 0 if q is None else q.shape[1]
+    dtype = dtype or k.dtype
+    if dtype not in _STORE:
+        raise ValueError("dtype must be float32 or bfloat16")
+    desc = HeadsDesc(C.sizeof(HeadsDesc), Hq, Hkv, dh, _STORE[k.dtype], _STORE[dtype], eps)
+    rope, gq, gk = (_floats("rope_cos_sin", rope_cos_sin, device, dh // 2, 2), _floats("q_gain", q_gain, device, dh),
+                    _floats("k_gain", k_gain, device, dh))
+    pos = None if positions is None else _ints("positions", positions, device, T)
+    with _Launch(device, stream) as sp:
+        q_out = None if q is None else torch.empty(T, Hq, dh, dtype=dtype, device=device)
+        k_out = torch.empty(T, Hkv, dh, dtype=dtype, device=device)
+        if status is None:
+            status = torch.zeros(1, dtype=torch.int32, device=device)
+        _paged_check(lib, lib.phyai_norm_rope_heads(C.addressof(desc), T, _ptr(q), q_row, k.data_ptr(), k_row, pos, rope,
+                                                    0 if rope is None else rope_cos_sin.shape[0], gq, gk, _ptr(q_out), k_out.data_ptr(),
+                                                    _ints("status", status, device, 1), sp))
+    return q_out, k_out
+
+
+class PagedCache:
+    """Pages of keys and values of every layer: ``pages`` ``[L, 2, n_pages * page_size, Hkv, dh]`` (the caller's, float32 or bfloat16).
+    A call's requests: ``cu_q_lens`` int32 ``[B + 1]`` (rows of the new tokens), ``kv_lens`` int32 ``[B]`` (cached tokens with the new
+    ones), ``page_table`` int32 ``[B, max_pages]``; see ``phyai.h``.  What a call finds wrong on the device raises the cache's status word
+    (``poll_status``), and later calls write nothing until it has been read.  Streams: calls on the cache are ordered by the caller."""
+
+    def __init__(self, pages: torch.Tensor, page_size: int):
+        self.lib = load_library()
+        if pages.dim() != 5 or pages.shape[1] != 2 or pages.dtype not in _STORE or not pages.is_cuda or not pages.is_contiguous():
+            raise ValueError("pages must be a contiguous float32 or bfloat16 CUDA tensor [L, 2, n_pages * page_size, Hkv, dh]")
+        L, _, rows, self.n_kv_heads, self.head_dim = pages.shape
+        if page_size <= 0 or rows % page_size:
+            raise ValueError("the pool's rows must be a multiple of page_size")
+        self.pages, self.page_size, self.n_layers, self.n_pages, self.device = pages, page_size, L, rows // page_size, pages.device
+        self.dtype = pages.dtype
+        self._desc = PagedCacheDesc(C.sizeof(PagedCacheDesc), L, self.n_kv_heads, self.head_dim, page_size, _STORE[pages.dtype], rows // page_size,
+                                    pages.data_ptr())
+        self._desc_ptr = C.addressof(self._desc)
+        self.status = torch.zeros(1, dtype=torch.int32, device=pages.device)
+        self._status_ptr = self.status.data_ptr()
+
+    def poll_status(self) -> int:
+        """Read-and-clear the status word (synchronises); returns the status code."""
+        st = int(self.status.item())
+        if st:
+            self.status.zero_()
+        return st
+
+    def _requests(self, cu_q_lens, kv_lens, page_table):
+        if page_table.dim() != 2:
+            raise ValueError("page_table must be [batch, max_pages]")
+        B, most = page_table.shape
+        cu = None if cu_q_lens is None else _ints("cu_q_lens", cu_q_lens, self.device, B + 1)
+        return B, most, cu, _ints("kv_lens", kv_lens, self.device, B), _ints("page_table", page_table, self.device, B, most)
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, cu_q_lens: torch.Tensor, kv_lens: torch.Tensor, page_table: torch.Tensor,
+               rope_cos_sin: Optional[torch.Tensor], k_gain: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+               q_gain: Optional[torch.Tensor] = None, eps: float = 1e-6, positions: Optional[torch.Tensor] = None, stream=None):
+        """New keys (normed with gain ``1 + k_gain`` unless None, rotated) and values ``[T, Hkv, dh]`` into the pages of ``layer``; with
+        ``q`` ``[T, Hq, dh]`` returns its normed, rotated rows in the cache's type (rows of no request are not written), else None."""
+        lib, device = self.lib, self.device
+        k_row, v_row = _head_rows("k", k, device), _head_rows("v", v, device, k)
+        q_row = 0 if q is None else _head_rows("q", q, device, k)
+        T, Hkv, dh = k.shape
+        if v.shape[1] != Hkv:
+            raise ValueError("k and v differ in heads")
+        Hq = 0 if q is None else q.shape[1]
+        desc = HeadsDesc(C.sizeof(HeadsDesc), Hq, Hkv, dh, _STORE[k.dtype], _STORE[self.dtype], eps)
+        B, most, cu, lens, table = self._requests(cu_q_lens, kv_lens, page_table)
+        rope, gq, gk = (_floats("rope_cos_sin", rope_cos_sin, device, dh // 2, 2), _floats("q_gain", q_gain, device, dh),
+                        _floats("k_gain", k_gain, device, dh))
+        pos = None if positions is None else _ints("positions", positions, device, T)
+        with _Launch(device, stream) as sp:
+            q_out = None if q is None else torch.empty(T, Hq, dh, dtype=self.dtype, device=device)
+            _paged_check(lib, lib.phyai_append_paged_kv(self._desc_ptr, C.addressof(desc), layer, T, _ptr(q), q_row, k.data_ptr(), k_row,
+                                                        v.data_ptr(), v_row, B, cu, lens, table, most, pos, rope,
+                                                        0 if rope is None else rope_cos_sin.shape[0], gq, gk, _ptr(q_out), self._status_ptr, sp))
+        return q_out
+
+    def attend(self, layer: int, q: torch.Tensor, cu_q_lens: torch.Tensor, kv_lens: torch.Tensor, page_table: torch.Tensor, causal: bool = True,
+               prefix_lens: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Attention of the new tokens' queries ``[T, Hq, dh]`` (rotated, the cache's type) over the pages of ``layer``, the tokens' own keys
+        included.  ``causal``: a token sees what is cached before it and itself, and with ``prefix_lens`` (int32 ``[B]``) the first so many
+        tokens.  Returns ``out`` ``[T, Hq, dh]`` (rows of no request are not written)."""
+        lib, device = self.lib, self.device
+        row = _head_rows("q", q, device)
+        T, Hq, dh = q.shape
+        if q.dtype != self.dtype or dh != self.head_dim:
+            raise ValueError("q and the cache differ in type or head_dim")
+        B, most, cu, lens, table = self._requests(cu_q_lens, kv_lens, page_table)
+        prefix = None if prefix_lens is None else _ints("prefix_lens", prefix_lens, device, B)
+        if out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != device or not out.is_contiguous()):
+            raise ValueError("out must be a contiguous tensor of q's shape and type")
+        if scale is not None and not scale > 0.0:
+            raise ValueError("scale must be positive")
+        with _Launch(device, stream) as sp:
+            need = lib.phyai_paged_attention_workspace_bytes(self._desc_ptr, Hq, T, B, most)
+            work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+            if out is None:
+                out = torch.empty(T, Hq, dh, dtype=q.dtype, device=device)
+            _paged_check(lib, lib.phyai_paged_attention(self._desc_ptr, layer, Hq, T, q.data_ptr(), row, B, cu, lens, table, most, 1 if causal else 0,
+                                                        prefix, 0.0 if scale is None else scale, out.data_ptr(), _ptr(work), need,
+                                                        self._status_ptr, sp))
+        return out
+
+    def pack(self, page_table: torch.Tensor, kv_lens: torch.Tensor, kv_tokens: int, out: Optional[torch.Tensor] = None, stream=None):
+        """The requests' cached tokens as the ragged prefix cache of ``Expert.denoise_batched``: (``prefix_kv`` ``[L, 2, kv_tokens, Hkv,
+        dh]``, ``cu_prefix_lens`` int32 ``[B + 1]``).  ``kv_tokens``: rows of it, at least the sum of ``kv_lens`` (rows past that are not
+        written)."""
+        lib, device = self.lib, self.device
+        B, most, _, lens, table = self._requests(None, kv_lens, page_table)
+        shape = (self.n_layers, 2, kv_tokens, self.n_kv_heads, self.head_dim)
+        if out is not None and (out.shape != shape or out.dtype != self.dtype or out.device != device or not out.is_contiguous()):
+            raise ValueError("out must be a contiguous tensor [L, 2, kv_tokens, Hkv, dh] of the cache's type")
+        with _Launch(device, stream) as sp:
+            if out is None:
+                out = torch.empty(shape, dtype=self.dtype, device=device)
+            cu = torch.empty(B + 1, dtype=torch.int32, device=device)
+            _paged_check(lib, lib.phyai_pack_paged_kv(self._desc_ptr, B, lens, table, most, out.data_ptr(), kv_tokens, cu.data_ptr(), self._status_ptr, sp))
+        return out, cu
 
 
 class Batcher:

@@ -1,0 +1,132 @@
+// Paged cache of keys and values: what its operators share (paged_heads.cu writes and drains it, paged_attention*.cu read it).
+//
+// The pool is [n_layers][2 (K, V)][n_pages * page_size][n_kv_heads][head_dim], head_dim contiguous: the layout of the denoising
+// loop's prefix cache, so that one page number serves all layers and both planes.  Cached token t of request b is row
+// table[b][t / page_size] * page_size + t % page_size of every plane.  Requests are ragged: request b's new tokens are rows
+// cu[b] .. cu[b + 1] - 1 of a call's token rows, its cache holds kv_lens[b] tokens of which the new ones are the last.
+#pragma once
+
+#include "../../include/phyai.h"
+#include "kernels.h"
+#include "ptx.cuh"
+
+namespace phyai {
+
+constexpr int PAGED_MAX_BATCH = 1024;
+
+struct PagedBatch {
+  const int* cu;          // [batch + 1]
+  const int* kv_lens;     // [batch]
+  const int* table;       // [batch][max_pages]
+  int batch, tokens, max_pages;
+  int page_shift;         // log2(page_size)
+  int n_pages;
+};
+
+// row of the planes that holds cached token t of request b, or -1 if its table entry names no page
+__device__ __forceinline__ long long paged_row(const PagedBatch& p, int b, int t) {
+  const int page = p.table[(size_t)b * p.max_pages + (t >> p.page_shift)];
+  if ((unsigned)page >= (unsigned)p.n_pages) return -1;
+  return ((long long)page << p.page_shift) + (t & ((1 << p.page_shift) - 1));
+}
+
+// Whether entry i of the lengths is in order (i = 0 .. batch - 1): the token rows do not go backwards or past the call's, the
+// cached tokens fit the table, and (append) the new ones are among them.
+__device__ __forceinline__ bool paged_entry_bad(const PagedBatch& p, int i, int lo, int hi, int kv, bool new_in_cache) {
+  return lo < 0 || hi < lo || hi > p.tokens || kv < 0 || (long long)kv > ((long long)p.max_pages << p.page_shift) || (new_in_cache && hi - lo > kv);
+}
+
+// Attention over the pages: row r of a request's packed rows is its new token r / group at query head kv_head * group + r % group
+// (the query heads that share a kv head stand together, so that they share the keys that a tile fetches).
+struct PagedAttn {
+  PagedBatch pb;
+  const void* q;          // [tokens] rows of hq heads, q_stride elements apart
+  long long q_stride;
+  void* out;              // [tokens][hq][dh]
+  const void *k_plane, *v_plane;
+  int plane;              // of K, among all planes of the pool (V: the next one)
+  const int* prefix_lens; // [batch] or null
+  int causal, hq, hkv, group;
+  float scale_log2;       // softmax scale * log2(e)
+  int ranges;             // most key ranges of a row
+  float* part_o;          // [ranges][tokens][hq][dh]: unnormalised accumulators of a key range
+  float4* part_ml;        // [ranges][tokens][hq]: maximum (log2 units), sum, ranges of this row (in range 0's entry)
+  int* status;
+  unsigned wait_limit;
+};
+
+// A request's lengths, and how many keys its new token i sees: keys [0, limit).
+struct PagedRequest {
+  int b, lo, n, kv, prefix;
+  __device__ __forceinline__ int limit(int i, int causal) const { return causal ? min(kv, max(max(kv - n + i + 1, prefix), 0)) : kv; }
+};
+
+// Request and row tile of unit `unit` (tiles of RT packed rows, requests in order); also whether every length of the call is in
+// order.  By a whole warp; r.b = -1: there are fewer units.
+template <int RT>
+__device__ __forceinline__ bool paged_unit(const PagedAttn& a, int unit, PagedRequest& r, int& tile) {
+  const int lane = threadIdx.x & 31;
+  bool bad = false;
+  int acc = 0;
+  r.b = -1, r.lo = r.n = r.kv = r.prefix = 0, tile = 0;
+  for (int i0 = 0; i0 < a.pb.batch; i0 += 32) {
+    const int i = i0 + lane;
+    int lo = 0, hi = 0, kv = 0;
+    if (i < a.pb.batch) {
+      lo = a.pb.cu[i], hi = a.pb.cu[i + 1], kv = a.pb.kv_lens[i];
+      bad |= paged_entry_bad(a.pb, i, lo, hi, kv, false);
+    }
+    const int n = bad ? 0 : ((hi - lo) * a.group + RT - 1) / RT;
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, acc + incl > unit);
+    if (r.b < 0 && hit) {
+      const int src = __ffs(hit) - 1;
+      r.b = i0 + src, r.lo = __shfl_sync(0xffffffffu, lo, src), r.n = __shfl_sync(0xffffffffu, hi, src) - r.lo;
+      r.kv = __shfl_sync(0xffffffffu, kv, src);
+      tile = unit - acc - __shfl_sync(0xffffffffu, incl - n, src);
+    }
+    acc += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (__any_sync(0xffffffffu, bad)) return false;
+  if (r.b >= 0 && a.prefix_lens) r.prefix = min(max(a.prefix_lens[r.b], 0), r.kv);
+  return true;
+}
+
+// One row over keys [k0, k1) of its request, key by key: the result of rows whose tile's products met an infinity or a NaN of a key
+// that the row does not see (0 x infinity).  By a whole warp; lane: channels lane * DH / 32 on.  o is unnormalised.
+template <int DH, typename T>
+__device__ __noinline__ void paged_row_alone(const PagedAttn& a, int b, const T* q, int hk, int k0, int k1, float* o, float& m, float& l) {
+  constexpr int C = DH / 32;
+  const int c = (threadIdx.x & 31) * C;
+  float x[C];
+#pragma unroll
+  for (int i = 0; i < C; ++i) x[i] = to_float(q[c + i]), o[i] = 0.f;
+  m = -INFINITY, l = 0.f;
+  for (int k = k0; k < k1; ++k) {
+    const long long row = paged_row(a.pb, b, k);
+    if (row < 0) continue;
+    const size_t at = ((size_t)row * a.hkv + hk) * DH + c;
+    const T *kp = (const T*)a.k_plane + at, *vp = (const T*)a.v_plane + at;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) s = fmaf(x[i], to_float(kp[i]), s);
+    s = warp_sum(s) * a.scale_log2;
+    const float mn = fmaxf(m, s), sub = mn == -INFINITY ? 0.f : mn, corr = exp2f(m - sub), p = exp2f(s - sub);
+    l = fmaf(l, corr, p), m = mn;
+#pragma unroll
+    for (int i = 0; i < C; ++i) o[i] = fmaf(p, to_float(vp[i]), o[i] * corr);
+  }
+}
+
+// The checks that every operator on a paged cache makes of it and of a call's requests (message in g_paged_err).
+extern thread_local char g_paged_err[256];
+phyai_status_t check_paged(const phyai_paged_cache_t* c, uint32_t layer, uint32_t batch, const int32_t* cu, const int32_t* kv_lens,
+                           const int32_t* table, uint32_t max_pages, uint32_t tokens, bool all_layers, PagedBatch* out);
+int paged_sm_count();
+
+}  // namespace phyai

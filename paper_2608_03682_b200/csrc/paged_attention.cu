@@ -1,0 +1,606 @@
+// Attention of new tokens over a paged cache (phyai_paged_attention): entry point, the kernel for few rows, the fp32 kernel and the
+// merge of key ranges.
+//
+// Row (token i, head h) of a request sees keys [0, limit(i)); o = sum_k p_k v_k / sum_k p_k, p_k = 2^(scale log2(e) (q k_k - max)).
+// Statistics and accumulators are fp32; P is rounded to bf16 (2^-9 of each weight, below the rounding of the bf16 output's terms) because
+// it is an operand of the tensor cores; the fp32 cache keeps everything fp32.
+//
+// Few rows (one token of a request is `group` rows): the cache is read once and nothing is reused, so memory bounds it.  Every warp
+// walks 16-key tiles of its own through its own ring of TMA copies, without any barrier between warps:
+//   S^T = K Q^T      mma.sync m16n8k16: keys are the 16 rows, 8 query rows the columns, so that 8 rows (pi0: the 8 heads of a token)
+//                    fill the instruction; as Q K^T half of it would be empty
+//   P^T              transposed in registers (movmatrix) into the B operand of
+//   O^T += V^T P^T   V^T by transposing ldmatrix
+// The warps of a block merge through shared memory, the blocks of a row (key ranges) through a second kernel.
+#include <cstdio>
+
+#include "paged.cuh"
+#include "attention.cuh"
+#include "tmap.h"
+
+namespace phyai {
+namespace {
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int row, int block, int plane, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(block), "r"(plane), "r"(bar)
+      : "memory");
+}
+
+// Key ranges of a row tile: at least `least` tiles of keys each.
+__device__ __forceinline__ int ranges_of(int tiles, int most, int least) { return max(1, min(most, tiles / least)); }
+
+// =============================================================================================
+// few rows, bf16
+// =============================================================================================
+constexpr int FW = 4;                    // warps of a block
+template <int DH>
+struct Few {
+  static constexpr int STAGES = DH == 256 ? 3 : DH == 128 ? 5 : 8;
+  static constexpr int TILE = 16 * DH * 2;                 // 16 keys (or values): blocks of 64 channels [DH / 64][16][128 B], swizzled
+  static constexpr int RING = STAGES * 2 * TILE;           // per warp
+  static constexpr size_t SMEM = 1024 + (size_t)FW * RING;
+};
+constexpr int FEW_LEAST = 2 * FW;        // tiles of 16 keys in a range, at least
+
+template <int DH, int NT>
+__global__ void __launch_bounds__(FW * 32) k_paged_few(const PagedAttn a, const __grid_constant__ CUtensorMap map) {
+  using F = Few<DH>;
+  constexpr int RT = 8 * NT, KS = DH / 16, ST = F::STAGES;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t full[FW][ST];
+  __shared__ float s_m[FW][RT], s_l[FW][RT];
+  __shared__ int abort_flag, s_again[RT];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int hk = blockIdx.y;
+  const uint32_t ring = ((smem_u32(smem_raw) + 1023u) & ~1023u) + (uint32_t)warp * F::RING;
+  pdl_launch_dependents();
+  if (threadIdx.x == 0) abort_flag = 0;
+  if (lane == 0) {
+    for (int i = 0; i < ST; ++i) mbar_init(smem_u32(&full[warp][i]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (threadIdx.x < RT) s_again[threadIdx.x] = 0;
+  __syncthreads();
+  pdl_wait();
+  const WaitCtx wc{a.status, &abort_flag, a.wait_limit};
+  PagedRequest r;
+  int tile;
+  const bool skip = status_set(a.status);
+  if (!paged_unit<RT>(a, blockIdx.x, r, tile)) {
+    if (threadIdx.x == 0) atomicExch(a.status, ST_INVALID_ARG);
+    return;
+  }
+  if (r.b < 0 || skip) return;
+  const int rows = min(RT, r.n * a.group - tile * RT), row0 = tile * RT;
+  const int n_keys = r.limit((row0 + rows - 1) / a.group, a.causal);              // (limits grow with the row)
+  const int tiles = (n_keys + 15) >> 4, ranges = ranges_of(tiles, a.ranges, FEW_LEAST), range = blockIdx.z;
+  if (range >= ranges) return;
+  const int t0 = (int)((long long)tiles * range / ranges), t1 = (int)((long long)tiles * (range + 1) / ranges);
+  const int mine = (t1 - t0 - warp + FW - 1) / FW;                                // tiles t0 + warp, + FW, ...
+
+  // ---- copies: one of K, one of V per tile.  Table entries come 32 tiles at a time, one per lane.
+  const size_t trow = (size_t)r.b * a.pb.max_pages;
+  int page_of = 0;
+  auto fetch_pages = [&](int i0) {
+    const int i = i0 + lane;
+    page_of = i < mine ? a.pb.table[trow + ((t0 + warp + i * FW) << 4 >> a.pb.page_shift)] : 0;
+    if ((unsigned)page_of >= (unsigned)a.pb.n_pages) {
+      atomicExch(a.status, ST_INVALID_ARG);
+      page_of = a.pb.n_pages;                                                     // (past the planes: the copy fills in zeros)
+    }
+  };
+  auto issue = [&](int i) {
+    if ((i & 31) == 0) fetch_pages(i);
+    const int page = __shfl_sync(0xffffffffu, page_of, i & 31);
+    if (lane == 0) {
+      const int key = (t0 + warp + i * FW) << 4, st = i % ST;
+      const int row = (int)(((long long)page << a.pb.page_shift) + (key & ((1 << a.pb.page_shift) - 1)));
+      const uint32_t bar = smem_u32(&full[warp][st]), dst = ring + (uint32_t)st * (2 * F::TILE);
+      mbar_expect_tx(bar, 2 * F::TILE);
+      tma_rows(dst, &map, row, hk * (DH / 64), a.plane, bar);
+      tma_rows(dst + F::TILE, &map, row, hk * (DH / 64), a.plane + 1, bar);
+    }
+  };
+  for (int i = 0; i < min(ST, mine); ++i) issue(i);
+
+  // ---- Q^T as B operand: lane (g, t) holds channels 16 kk + 2 t, + 1 and + 8, + 9 of row g
+  uint32_t qf[NT][KS][2];
+  int lim[NT][2], min_lim = 0x7fffffff;            // of rows 2 t and 2 t + 1
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int rr = nt * 8 + g;
+    const bool live = rr < rows;
+    const int i = (row0 + rr) / a.group, h = hk * a.group + (row0 + rr) % a.group;
+    const uint32_t* qp = reinterpret_cast<const uint32_t*>((const __nv_bfloat16*)a.q + (live ? (r.lo + i) * a.q_stride + (long long)h * DH : 0)) + t;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      qf[nt][kk][0] = live ? qp[kk * 8] : 0u;
+      qf[nt][kk][1] = live ? qp[kk * 8 + 4] : 0u;
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int re = nt * 8 + 2 * t + e;
+      lim[nt][e] = re < rows ? r.limit((row0 + re) / a.group, a.causal) : n_keys;
+      min_lim = min(min_lim, lim[nt][e]);
+    }
+  }
+  min_lim = __reduce_min_sync(0xffffffffu, min_lim);
+
+  float acc[NT][KS][4] = {}, m[NT][2], l[NT][2] = {};
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = -INFINITY;
+  const int rowk = lane & 15, chk = lane >> 4;                       // ldmatrix of K: keys 0-15, chunks 2 kk, 2 kk + 1
+  const int rowv = (lane & 7) + ((lane >> 4) << 3), chv = (lane >> 3) & 1;   // of V: (keys 0-7, ch 0-7), (0-7, 8-15), (8-15, 0-7), (8-15, 8-15)
+  for (int it = 0; it < mine; ++it) {
+    const int st = it % ST, key0 = (t0 + warp + it * FW) << 4;
+    const uint32_t ks = ring + (uint32_t)st * (2 * F::TILE), vs = ks + F::TILE;
+    mbar_wait_drain(smem_u32(&full[warp][st]), (uint32_t)(it / ST) & 1u, wc);
+    if (key0 + 16 > r.kv) {                                          // rows past the cached tokens hold anything: their values become zeros
+      const int keep = r.kv - key0;
+      for (int i = lane; i < (16 - keep) * (DH / 8); i += 32) {
+        const int row = keep + i / (DH / 8), ch = i % (DH / 8);
+        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(vs + (uint32_t)((ch >> 3) * 2048 + row * 128 + (ch & 7) * 16)), "r"(0u) : "memory");
+      }
+      __syncwarp();
+    }
+    float s[NT][2][4] = {};
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      uint32_t kf[4];
+      const int ch = 2 * kk + chk;
+      ldsm_x4(ks + (uint32_t)((ch >> 3) * 2048 + rowk * 128 + (((ch & 7) ^ (rowk & 7)) << 4)), kf[0], kf[1], kf[2], kf[3]);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) mma_bf16(s[nt][kk & 1], kf, qf[nt][kk][0], qf[nt][kk][1]);
+    }
+    uint32_t pf[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (s[nt][0][e] + s[nt][1][e]) * a.scale_log2;
+      if (key0 + 16 > min_lim) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = key0 + g + (e >> 1) * 8 < lim[nt][e & 1] ? x[e] : -INFINITY;
+      }
+      float mx[2], corr[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        mx[e] = fmaxf(x[e], x[e + 2]);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], o));
+        const float mn = fmaxf(m[nt][e], mx[e]), sub = mn == -INFINITY ? 0.f : mn;
+        corr[e] = ex2_fast(m[nt][e] - sub);
+        x[e] = ex2_fast(x[e] - sub), x[e + 2] = ex2_fast(x[e + 2] - sub);
+        l[nt][e] = l[nt][e] * corr[e] + x[e] + x[e + 2];
+        m[nt][e] = mn;
+      }
+      if (__any_sync(0xffffffffu, corr[0] != 1.0f || corr[1] != 1.0f)) {
+#pragma unroll
+        for (int ct = 0; ct < KS; ++ct) acc[nt][ct][0] *= corr[0], acc[nt][ct][1] *= corr[1], acc[nt][ct][2] *= corr[0], acc[nt][ct][3] *= corr[1];
+      }
+      pf[nt][0] = transpose8x8(pack_bf16(x[0], x[1]));
+      pf[nt][1] = transpose8x8(pack_bf16(x[2], x[3]));
+    }
+#pragma unroll
+    for (int ct = 0; ct < KS; ++ct) {
+      uint32_t vf[4];
+      const int ch = 2 * ct + chv;
+      ldsm_x4_t(vs + (uint32_t)((ch >> 3) * 2048 + rowv * 128 + (((ch & 7) ^ (rowv & 7)) << 4)), vf[0], vf[1], vf[2], vf[3]);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) mma_bf16(acc[nt][ct], vf, pf[nt][0], pf[nt][1]);
+    }
+    __syncwarp();
+    if (it + ST < mine) issue(it + ST);
+  }
+
+  // ---- the warps' results: rows of DH fp32 (4 more: free of bank conflicts) in each warp's own ring
+  constexpr int PITCH = DH + 4;
+  static_assert(RT * PITCH * 4 <= F::RING, "a warp's partial result exceeds its ring");
+  float* const part = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
+  float* const part0 = reinterpret_cast<float*>(smem_raw + (ring - (uint32_t)warp * F::RING - smem_u32(smem_raw)));
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], o);
+      if (g == 0) s_m[warp][nt * 8 + 2 * t + e] = m[nt][e], s_l[warp][nt * 8 + 2 * t + e] = l[nt][e];
+    }
+#pragma unroll
+    for (int ct = 0; ct < KS; ++ct)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[(nt * 8 + 2 * t + (e & 1)) * PITCH + ct * 16 + g + (e >> 1) * 8] = acc[nt][ct][e];
+  }
+  __syncthreads();
+  if (*reinterpret_cast<volatile int*>(&abort_flag)) return;
+  for (int i = threadIdx.x; i < rows * (DH / 4); i += FW * 32) {
+    const int rr = i / (DH / 4), c = (i % (DH / 4)) * 4;
+    float M = -INFINITY, w[FW], sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < FW; ++k) M = fmaxf(M, s_m[k][rr]);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < FW; ++k) {
+      w[k] = s_m[k][rr] == -INFINITY ? 0.f : ex2_fast(s_m[k][rr] - M);
+      sum += w[k] * s_l[k][rr];
+      const float4 v = *reinterpret_cast<const float4*>(part0 + (size_t)k * (F::RING / 4) + rr * PITCH + c);
+      o.x += w[k] * v.x, o.y += w[k] * v.y, o.z += w[k] * v.z, o.w += w[k] * v.w;
+    }
+    // (0 x infinity and 0 x NaN of keys that this row does not see, or of its own: told apart below)
+    if (a.causal && !(fabsf(o.x) + fabsf(o.y) + fabsf(o.z) + fabsf(o.w) < INFINITY)) s_again[rr] = 1;
+    const int tok = r.lo + (row0 + rr) / a.group, h = hk * a.group + (row0 + rr) % a.group;
+    if (ranges == 1) {
+      const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+      *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + ((size_t)tok * a.hq + h) * DH + c) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    } else {
+      *reinterpret_cast<float4*>(a.part_o + (((size_t)range * a.pb.tokens + tok) * a.hq + h) * DH + c) = o;
+    }
+    if (c == 0 && a.ranges > 1) a.part_ml[((size_t)range * a.pb.tokens + tok) * a.hq + h] = make_float4(M, sum, (float)ranges, 0.f);
+  }
+  if (!a.causal) return;
+  __syncthreads();
+  for (int rr = warp; rr < rows; rr += FW) {
+    if (!s_again[rr]) continue;
+    const int i = (row0 + rr) / a.group, tok = r.lo + i, h = hk * a.group + (row0 + rr) % a.group, c = lane * (DH / 32);
+    float o[DH / 32], M, sum;
+    paged_row_alone<DH>(a, r.b, (const __nv_bfloat16*)a.q + tok * a.q_stride + (long long)h * DH, hk, t0 * 16, min(t1 * 16, r.limit(i, 1)), o, M, sum);
+    const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+#pragma unroll
+    for (int e = 0; e < DH / 32; ++e) {
+      if (ranges == 1) ((__nv_bfloat16*)a.out)[((size_t)tok * a.hq + h) * DH + c + e] = __float2bfloat16_rn(o[e] * inv);
+      else a.part_o[(((size_t)range * a.pb.tokens + tok) * a.hq + h) * DH + c + e] = o[e];
+    }
+    if (lane == 0 && ranges > 1) a.part_ml[((size_t)range * a.pb.tokens + tok) * a.hq + h] = make_float4(M, sum, (float)ranges, 0.f);
+  }
+}
+
+// =============================================================================================
+// fp32
+// =============================================================================================
+constexpr int XT = 128, XK = 32;         // threads; keys per tile
+constexpr int F32_LEAST = 2;             // tiles of keys in a range, at least
+
+// A thread takes RR rows and, of them, 4 of a tile's 32 logits and DH / 8 of the accumulator's channels; the 8 threads of a row are
+// neighbours in a warp, so that P and the statistics cross lanes by shuffles and a warp's own shared memory.
+template <int DH, int RR>
+__global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
+  constexpr int RT = 16 * RR, PITCH = DH + 4, PP = XK + 4, CJ = DH / 32;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  float* const Q = reinterpret_cast<float*>(smem_raw);
+  float *const K = Q + RT * PITCH, *const V = K + XK * PITCH, *const P = V + XK * PITCH;
+  const int tid = threadIdx.x, rg = tid >> 3, kg = tid & 7, lane = tid & 31, warp = tid >> 5;
+  const int hk = blockIdx.y;
+  pdl_launch_dependents();
+  pdl_wait();
+  PagedRequest r;
+  int tile;
+  const bool skip = status_set(a.status);
+  if (!paged_unit<RT>(a, blockIdx.x, r, tile)) {
+    if (tid == 0) atomicExch(a.status, ST_INVALID_ARG);
+    return;
+  }
+  if (r.b < 0 || skip) return;
+  const int rows = min(RT, r.n * a.group - tile * RT), row0 = tile * RT;
+  const int n_keys = r.limit((row0 + rows - 1) / a.group, a.causal);
+  const int tiles = (n_keys + XK - 1) / XK, ranges = ranges_of(tiles, a.ranges, F32_LEAST), range = blockIdx.z;
+  if (range >= ranges) return;
+  const int t0 = (int)((long long)tiles * range / ranges), t1 = (int)((long long)tiles * (range + 1) / ranges);
+  for (int i = tid; i < RT * (DH / 4); i += XT) {
+    const int rr = i / (DH / 4), c = (i % (DH / 4)) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (rr < rows) v = *reinterpret_cast<const float4*>((const float*)a.q + (r.lo + (row0 + rr) / a.group) * a.q_stride + (long long)(hk * a.group + (row0 + rr) % a.group) * DH + c);
+    *reinterpret_cast<float4*>(Q + rr * PITCH + c) = v;
+  }
+  float acc[RR][CJ][4] = {}, m[RR], l[RR] = {};
+  int lim[RR];
+#pragma unroll
+  for (int i = 0; i < RR; ++i) {
+    const int rr = rg + 16 * i;
+    m[i] = -INFINITY, lim[i] = rr < rows ? r.limit((row0 + rr) / a.group, a.causal) : n_keys;
+  }
+  bool bad_page = false;
+  for (int kt = t0; kt < t1; ++kt) {
+    __syncthreads();
+    for (int i = tid; i < 2 * XK * (DH / 4); i += XT) {
+      const int is_v = i >= XK * (DH / 4), j = i - is_v * XK * (DH / 4), kr = j / (DH / 4), c = (j % (DH / 4)) * 4, key = kt * XK + kr;
+      long long row = -1;
+      if (key < n_keys) {
+        row = paged_row(a.pb, r.b, key);
+        bad_page |= row < 0;
+      }
+      const float* src = (const float*)(is_v ? a.v_plane : a.k_plane);
+      cp_async16(smem_u32((is_v ? V : K) + kr * PITCH + c), row >= 0 ? src + ((size_t)row * a.hkv + hk) * DH + c : src, row >= 0 ? 16u : 0u);
+    }
+    cp_async_commit();
+    cp_async_wait<0>();
+    __syncthreads();
+    float s[RR][4] = {};
+#pragma unroll 4
+    for (int d = 0; d < DH; d += 4) {
+      float4 kv[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4*>(K + (kg + 8 * j) * PITCH + d);
+#pragma unroll
+      for (int i = 0; i < RR; ++i) {
+        const float4 qv = *reinterpret_cast<const float4*>(Q + (rg + 16 * i) * PITCH + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] = fmaf(qv.x, kv[j].x, fmaf(qv.y, kv[j].y, fmaf(qv.z, kv[j].z, fmaf(qv.w, kv[j].w, s[i][j]))));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < RR; ++i) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[i][j] = kt * XK + kg + 8 * j < lim[i] ? s[i][j] * a.scale_log2 : -INFINITY;
+        mx = fmaxf(mx, s[i][j]);
+      }
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      const float mn = fmaxf(m[i], mx), sub = mn == -INFINITY ? 0.f : mn, corr = exp2f(m[i] - sub);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = exp2f(s[i][j] - sub);
+        P[(rg + 16 * i) * PP + kg + 8 * j] = p;
+        sum += p;
+      }
+      l[i] = l[i] * corr + sum, m[i] = mn;
+#pragma unroll
+      for (int j = 0; j < CJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] *= corr;
+    }
+    __syncwarp();
+#pragma unroll 2
+    for (int k = 0; k < XK; k += 4) {
+      float4 p[RR];
+#pragma unroll
+      for (int i = 0; i < RR; ++i) p[i] = *reinterpret_cast<const float4*>(P + (rg + 16 * i) * PP + k);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+#pragma unroll
+        for (int j = 0; j < CJ; ++j) {
+          const float4 v = *reinterpret_cast<const float4*>(V + (k + kk) * PITCH + kg * 4 + 32 * j);
+#pragma unroll
+          for (int i = 0; i < RR; ++i) {
+            const float w = kk == 0 ? p[i].x : kk == 1 ? p[i].y : kk == 2 ? p[i].z : p[i].w;
+            acc[i][j][0] = fmaf(w, v.x, acc[i][j][0]), acc[i][j][1] = fmaf(w, v.y, acc[i][j][1]);
+            acc[i][j][2] = fmaf(w, v.z, acc[i][j][2]), acc[i][j][3] = fmaf(w, v.w, acc[i][j][3]);
+          }
+        }
+      }
+    }
+  }
+  if (bad_page) atomicExch(a.status, ST_INVALID_ARG);
+#pragma unroll
+  for (int i = 0; i < RR; ++i) {
+    const int rr = rg + 16 * i;
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+    float fin = 0.f;
+#pragma unroll
+    for (int j = 0; j < CJ; ++j) fin += fabsf(acc[i][j][0]) + fabsf(acc[i][j][1]) + fabsf(acc[i][j][2]) + fabsf(acc[i][j][3]);
+    const unsigned odd = __ballot_sync(0xffffffffu, a.causal && rr < rows && !(fin < INFINITY));     // (see k_paged_few)
+    const int tok = r.lo + (row0 + rr) / a.group, h = hk * a.group + (row0 + rr) % a.group;
+    const size_t slot = ((size_t)range * a.pb.tokens + tok) * a.hq + h;
+    if (rr < rows) {
+      float* dst = ranges == 1 ? (float*)a.out + ((size_t)tok * a.hq + h) * DH : a.part_o + slot * DH;
+      const float inv = ranges > 1 ? 1.0f : l[i] > 0.f || l[i] != l[i] ? 1.0f / l[i] : 0.f;
+#pragma unroll
+      for (int j = 0; j < CJ; ++j)
+        *reinterpret_cast<float4*>(dst + kg * 4 + 32 * j) = make_float4(acc[i][j][0] * inv, acc[i][j][1] * inv, acc[i][j][2] * inv, acc[i][j][3] * inv);
+      if (kg == 0 && a.ranges > 1) a.part_ml[slot] = make_float4(m[i], l[i], (float)ranges, 0.f);
+    }
+    __syncwarp();
+    for (int z = 0; z < 4; ++z) {                        // the four rows of this warp
+      if (!(odd & (0xffu << (8 * z)))) continue;
+      const int r2 = warp * 4 + z + 16 * i, i2 = (row0 + r2) / a.group, tok2 = r.lo + i2, h2 = hk * a.group + (row0 + r2) % a.group;
+      float o[DH / 32], M, sum;
+      paged_row_alone<DH>(a, r.b, (const float*)a.q + tok2 * a.q_stride + (long long)h2 * DH, hk, t0 * XK, min(t1 * XK, r.limit(i2, 1)), o, M, sum);
+      const size_t slot2 = ((size_t)range * a.pb.tokens + tok2) * a.hq + h2;
+      float* dst = (ranges == 1 ? (float*)a.out + ((size_t)tok2 * a.hq + h2) * DH : a.part_o + slot2 * DH) + lane * (DH / 32);
+      const float inv = ranges > 1 ? 1.0f : sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+#pragma unroll
+      for (int e = 0; e < DH / 32; ++e) dst[e] = o[e] * inv;
+      if (lane == 0 && ranges > 1) a.part_ml[slot2] = make_float4(M, sum, (float)ranges, 0.f);
+    }
+  }
+}
+
+// =============================================================================================
+// merge of key ranges
+// =============================================================================================
+// A warp per row: weights 2^(m_r - max m), fixed order of the ranges.
+template <int DH, typename OUT>
+__global__ void __launch_bounds__(128) k_paged_merge(const PagedAttn a) {
+  constexpr int C = DH / 32;
+  const int lane = threadIdx.x & 31, c = lane * C;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5), rows = (long long)a.pb.tokens * a.hq;
+  pdl_launch_dependents();
+  pdl_wait();
+  if (status_set(a.status) || row >= rows) return;
+  const int tok = (int)(row / a.hq);
+  if (tok < a.pb.cu[0] || tok >= a.pb.cu[a.pb.batch]) return;
+  const int ranges = (int)a.part_ml[row].z;
+  if (ranges <= 1) return;
+  float M = -INFINITY;
+  for (int k = lane; k < ranges; k += 32) M = fmaxf(M, a.part_ml[(size_t)k * rows + row].x);
+  M = warp_max(M);
+  float o[C] = {}, sum = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < ranges; ++k) {
+    const float4 ml = a.part_ml[(size_t)k * rows + row];
+    const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+    sum = fmaf(w, ml.y, sum);
+    const float* p = a.part_o + ((size_t)k * rows + row) * DH + c;
+#pragma unroll
+    for (int e = 0; e < C; ++e) o[e] = fmaf(w, p[e], o[e]);
+  }
+  const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+  OUT* dst = (OUT*)a.out + row * DH + c;
+#pragma unroll
+  for (int e = 0; e < C; ++e) {
+    if constexpr (sizeof(OUT) == 4) dst[e] = o[e] * inv;
+    else dst[e] = __float2bfloat16_rn(o[e] * inv);
+  }
+}
+
+// =============================================================================================
+// host side
+// =============================================================================================
+phyai_status_t bad_arg(const char* m) {
+  snprintf(g_paged_err, sizeof(g_paged_err), "%s", m);
+  return PHYAI_ERR_INVALID_ARG;
+}
+
+// What a call launches: the kernel's row tile, its units and key ranges.
+struct Plan {
+  int f32, rt, units, ranges;
+};
+Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int max_pages, int n_sm) {
+  Plan p{};
+  const int group = hq / (int)c->n_kv_heads, holders = tokens < batch ? tokens : batch;      // requests with tokens, at most
+  const long long rows = (long long)tokens * group;
+  p.f32 = c->dtype == PHYAI_F32;
+  if (p.f32) {
+    p.rt = rows > 16ll * holders ? 64 : 16;
+  } else {
+    const int most = c->head_dim == 64 ? 32 : 16;
+    p.rt = rows <= 8ll * holders ? 8 : rows <= 16ll * holders || most == 16 ? 16 : most;
+  }
+  p.units = (int)(rows / p.rt) + holders;
+  // key ranges: enough blocks for two rounds of the SMs, of at least 128 keys
+  const long long full = (rows + p.rt - 1) / p.rt > holders ? (rows + p.rt - 1) / p.rt : holders, blocks = full * c->n_kv_heads;
+  const long long keys = (long long)max_pages * c->page_size;
+  long long ranges = (2ll * n_sm + blocks - 1) / blocks;
+  if (ranges > keys / 128) ranges = keys / 128;
+  p.ranges = (int)(ranges < 1 ? 1 : ranges > 64 ? 64 : ranges);
+  return p;
+}
+size_t partial_bytes(const Plan& p, int hq, int dh, int tokens) {
+  return p.ranges > 1 ? (size_t)p.ranges * tokens * hq * ((size_t)dh * 4 + 16) : 0;
+}
+
+template <typename K>
+cudaError_t allow_smem(K kern, size_t bytes) { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); }
+
+template <int DH, int NT>
+cudaError_t launch_few(const PagedAttn& a, const Plan& p, const CUtensorMap& map, cudaStream_t st) {
+  static PerDeviceOnce once;
+  if (once.needed()) {
+    const cudaError_t e = allow_smem(k_paged_few<DH, NT>, Few<DH>::SMEM);
+    if (e != cudaSuccess) return e;
+    once.done();
+  }
+  return launch_pdl(k_paged_few<DH, NT>, dim3(p.units, a.hkv, p.ranges), dim3(FW * 32), Few<DH>::SMEM, st, a, map);
+}
+template <int DH, int RR>
+cudaError_t launch_f32(const PagedAttn& a, const Plan& p, cudaStream_t st) {
+  constexpr size_t smem = ((size_t)(16 * RR + 2 * XK) * (DH + 4) + 16 * RR * (XK + 4)) * 4;
+  static PerDeviceOnce once;
+  if (once.needed()) {
+    const cudaError_t e = allow_smem(k_paged_f32<DH, RR>, smem);
+    if (e != cudaSuccess) return e;
+    once.done();
+  }
+  return launch_pdl(k_paged_f32<DH, RR>, dim3(p.units, a.hkv, p.ranges), dim3(XT), smem, st, a);
+}
+// the pool as rows of 64 channels: {64, rows of a plane, blocks of 64 channels in a row, planes}, copies of `box` rows of a head
+bool pool_map(CUtensorMap* m, const phyai_paged_cache_t* c, uint32_t box) {
+  const EncodeTiled enc = encode_tiled();
+  if (!enc) return false;
+  const cuuint64_t row = (cuuint64_t)c->n_kv_heads * c->head_dim * 2, rows = c->n_pages * c->page_size;
+  const cuuint64_t dims[4] = {64, rows, row / 128, 2ull * c->n_layers}, strides[3] = {row, 128, rows * row};
+  const cuuint32_t bx[4] = {64, box, c->head_dim / 64, 1}, es[4] = {1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, c->pages, dims, strides, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+}  // namespace phyai
+
+extern "C" {
+
+size_t phyai_paged_attention_workspace_bytes(const phyai_paged_cache_t* cache, uint32_t n_q_heads, uint32_t tokens, uint32_t batch,
+                                             uint32_t max_pages) {
+  using namespace phyai;
+  const int n_sm = paged_sm_count();
+  if (!cache || !cache->n_kv_heads || !n_q_heads || !tokens || !batch || n_sm <= 0) return 0;
+  return partial_bytes(make_plan(cache, (int)n_q_heads, (int)tokens, (int)batch, (int)max_pages, n_sm), (int)n_q_heads, (int)cache->head_dim, (int)tokens);
+}
+
+phyai_status_t phyai_paged_attention(const phyai_paged_cache_t* cache, uint32_t layer, uint32_t n_q_heads, uint32_t tokens, const void* q,
+                                     uint64_t q_stride, uint32_t batch, const int32_t* cu_q_lens, const int32_t* kv_lens,
+                                     const int32_t* page_table, uint32_t max_pages, uint32_t causal, const int32_t* prefix_lens, float scale,
+                                     void* out, void* workspace, size_t workspace_bytes, int32_t* status_word, void* stream) {
+  using namespace phyai;
+  PagedAttn a{};
+  const phyai_status_t s = check_paged(cache, layer, batch, cu_q_lens, kv_lens, page_table, max_pages, tokens, false, &a.pb);
+  if (s != PHYAI_OK) return s;
+  if (!status_word || (tokens && (!q || !out))) return bad_arg("a pointer argument is NULL");
+  if (!n_q_heads || n_q_heads % cache->n_kv_heads || n_q_heads > 65535u) return bad_arg("n_q_heads must be a multiple of the cache's n_kv_heads");
+  if (prefix_lens && !causal) return bad_arg("prefix_lens without the causal mask");
+  if (!(scale >= 0.f) || scale > 1e30f) return bad_arg("scale must be positive (0: 1 / sqrt(head_dim))");
+  const uint64_t es = cache->dtype == PHYAI_F32 ? 4 : 2;
+  if (q_stride < (uint64_t)n_q_heads * cache->head_dim || q_stride > (1ull << 40)) return bad_arg("a row stride is smaller than the row's heads, or too large");
+  if (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(workspace)) & 15u) || (q_stride * es) % 16)
+    return bad_arg("pointers and row strides must be multiples of 16 bytes");
+  if ((uint64_t)tokens * (n_q_heads / cache->n_kv_heads) > 0x7fffffffull) return bad_arg("tokens too large");
+  if (!tokens) return PHYAI_OK;
+  const int n_sm = paged_sm_count();
+  if (n_sm <= 0) {
+    snprintf(g_paged_err, sizeof(g_paged_err), "no CUDA device (there is no CPU fallback)");
+    return PHYAI_ERR_CUDA;
+  }
+  const int dh = (int)cache->head_dim;
+  const Plan p = make_plan(cache, (int)n_q_heads, (int)tokens, (int)batch, (int)max_pages, n_sm);
+  const size_t need = partial_bytes(p, (int)n_q_heads, dh, (int)tokens);
+  if (need && (!workspace || workspace_bytes < need)) {
+    snprintf(g_paged_err, sizeof(g_paged_err), "needs %zu bytes of workspace, %zu given", need, workspace ? workspace_bytes : (size_t)0);
+    return PHYAI_ERR_INVALID_ARG;
+  }
+  const size_t plane = (size_t)cache->n_pages * cache->page_size * cache->n_kv_heads * dh * es;
+  a.q = q, a.q_stride = (long long)q_stride, a.out = out, a.plane = (int)layer * 2;
+  a.k_plane = (const char*)cache->pages + 2 * (size_t)layer * plane, a.v_plane = (const char*)a.k_plane + plane;
+  a.prefix_lens = prefix_lens, a.causal = causal ? 1 : 0, a.hq = (int)n_q_heads, a.hkv = (int)cache->n_kv_heads, a.group = a.hq / a.hkv;
+  a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)dh)) * LOG2E;
+  a.ranges = p.ranges, a.status = status_word, a.wait_limit = 1u << 22;
+  a.part_ml = reinterpret_cast<float4*>(workspace), a.part_o = reinterpret_cast<float*>(a.part_ml + (size_t)p.ranges * tokens * n_q_heads);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaErrorInvalidValue;
+  if (p.f32) {
+    if (dh == 64) e = p.rt == 16 ? launch_f32<64, 1>(a, p, st) : launch_f32<64, 4>(a, p, st);
+    else if (dh == 128) e = p.rt == 16 ? launch_f32<128, 1>(a, p, st) : launch_f32<128, 4>(a, p, st);
+    else e = p.rt == 16 ? launch_f32<256, 1>(a, p, st) : launch_f32<256, 4>(a, p, st);
+  } else {
+    CUtensorMap map;
+    if (!pool_map(&map, cache, 16)) {
+      snprintf(g_paged_err, sizeof(g_paged_err), "cuTensorMapEncodeTiled failed");
+      return PHYAI_ERR_CUDA;
+    }
+    if (dh == 64) e = p.rt == 8 ? launch_few<64, 1>(a, p, map, st) : p.rt == 16 ? launch_few<64, 2>(a, p, map, st) : launch_few<64, 4>(a, p, map, st);
+    else if (dh == 128) e = p.rt == 8 ? launch_few<128, 1>(a, p, map, st) : launch_few<128, 2>(a, p, map, st);
+    else e = p.rt == 8 ? launch_few<256, 1>(a, p, map, st) : launch_few<256, 2>(a, p, map, st);
+  }
+  if (e == cudaSuccess && p.ranges > 1) {
+    const dim3 grid((unsigned)(((long long)tokens * n_q_heads + 3) / 4));
+    if (p.f32) e = dh == 64 ? launch_pdl(k_paged_merge<64, float>, grid, dim3(128), 0, st, a) : dh == 128 ? launch_pdl(k_paged_merge<128, float>, grid, dim3(128), 0, st, a) : launch_pdl(k_paged_merge<256, float>, grid, dim3(128), 0, st, a);
+    else e = dh == 64 ? launch_pdl(k_paged_merge<64, __nv_bfloat16>, grid, dim3(128), 0, st, a) : dh == 128 ? launch_pdl(k_paged_merge<128, __nv_bfloat16>, grid, dim3(128), 0, st, a) : launch_pdl(k_paged_merge<256, __nv_bfloat16>, grid, dim3(128), 0, st, a);
+  }
+  if (e == cudaSuccess) e = cudaGetLastError();
+  if (e != cudaSuccess) {
+    snprintf(g_paged_err, sizeof(g_paged_err), "paged attention launch failed: %s", cudaGetErrorString(e));
+    return PHYAI_ERR_CUDA;
+  }
+  return PHYAI_OK;
+}
+
+}  // extern "C"
