@@ -97,6 +97,20 @@ __device__ __forceinline__ bool paged_unit(const PagedAttn& a, int unit, PagedRe
   return true;
 }
 
+// Whether a value of keys [k0, k1) that a row does not see is infinite or NaN, in channels [c0, c0 + 32 C).  By a whole warp, C channels a lane.
+template <int C, typename T>
+__device__ __noinline__ bool paged_hidden_odd(const PagedAttn& a, int b, int hk, int dh, int c0, int k0, int k1) {
+  bool odd = false;
+  for (int k = k0; k < k1; ++k) {
+    const long long row = paged_row(a.pb, b, k);
+    if (row < 0) continue;
+    const T* v = (const T*)a.v_plane + ((size_t)row * a.hkv + hk) * dh + c0 + (threadIdx.x & 31) * C;
+#pragma unroll
+    for (int i = 0; i < C; ++i) odd |= !(fabsf(to_float(v[i])) < INFINITY);
+  }
+  return __any_sync(0xffffffffu, odd);
+}
+
 // One row over keys [k0, k1) of its request, key by key: the result of rows whose tile's products met an infinity or a NaN of a key
 // that the row does not see (0 x infinity).  By a whole warp; lane: channels lane * DH / 32 on.  o is unnormalised.
 template <int DH, typename T>
@@ -107,6 +121,7 @@ __device__ __noinline__ void paged_row_alone(const PagedAttn& a, int b, const T*
 #pragma unroll
   for (int i = 0; i < C; ++i) x[i] = to_float(q[c + i]), o[i] = 0.f;
   m = -INFINITY, l = 0.f;
+#pragma unroll 4
   for (int k = k0; k < k1; ++k) {
     const long long row = paged_row(a.pb, b, k);
     if (row < 0) continue;
@@ -128,5 +143,19 @@ extern thread_local char g_paged_err[256];
 phyai_status_t check_paged(const phyai_paged_cache_t* c, uint32_t layer, uint32_t batch, const int32_t* cu, const int32_t* kv_lens,
                            const int32_t* table, uint32_t max_pages, uint32_t tokens, bool all_layers, PagedBatch* out);
 int paged_sm_count();
+
+// Key ranges of a row tile: at least `least` tiles of keys each.
+__host__ __device__ __forceinline__ int ranges_of(int tiles, int most, int least) {
+  const int r = tiles / least < most ? tiles / least : most;
+  return r > 1 ? r : 1;
+}
+// the pool as rows of 64 channels: {64, rows of a plane, blocks of 64 channels in a row, planes}; a copy: `rows` rows, `blocks` blocks
+bool paged_pool_map(void* map, const phyai_paged_cache_t* c, uint32_t rows, uint32_t blocks);
+
+// many rows: paged_attention_pair.cu
+bool paged_pair_supported(int dh, int group);
+int paged_pair_tokens(int group);                       // tokens of a unit
+int paged_pair_resident(int dh);                        // pairs at a time (0 on an error)
+cudaError_t launch_paged_pair(const PagedAttn& a, const phyai_paged_cache_t* cache, long long items, cudaStream_t st);
 
 }  // namespace phyai

@@ -33,9 +33,6 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, i
       : "memory");
 }
 
-// Key ranges of a row tile: at least `least` tiles of keys each.
-__device__ __forceinline__ int ranges_of(int tiles, int most, int least) { return max(1, min(most, tiles / least)); }
-
 // =============================================================================================
 // few rows, bf16
 // =============================================================================================
@@ -248,7 +245,9 @@ __global__ void __launch_bounds__(FW * 32) k_paged_few(const PagedAttn a, const 
   __syncthreads();
   for (int rr = warp; rr < rows; rr += FW) {
     if (!s_again[rr]) continue;
-    const int i = (row0 + rr) / a.group, tok = r.lo + i, h = hk * a.group + (row0 + rr) % a.group, c = lane * (DH / 32);
+    const int i = (row0 + rr) / a.group, hidden = max(t0 * 16, r.limit(i, 1));
+    if (!paged_hidden_odd<DH / 32, __nv_bfloat16>(a, r.b, hk, DH, 0, hidden, min(t1 * 16, r.kv))) continue;
+    const int tok = r.lo + i, h = hk * a.group + (row0 + rr) % a.group, c = lane * (DH / 32);
     float o[DH / 32], M, sum;
     paged_row_alone<DH>(a, r.b, (const __nv_bfloat16*)a.q + tok * a.q_stride + (long long)h * DH, hk, t0 * 16, min(t1 * 16, r.limit(i, 1)), o, M, sum);
     const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
@@ -402,7 +401,9 @@ __global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
     __syncwarp();
     for (int z = 0; z < 4; ++z) {                        // the four rows of this warp
       if (!(odd & (0xffu << (8 * z)))) continue;
-      const int r2 = warp * 4 + z + 16 * i, i2 = (row0 + r2) / a.group, tok2 = r.lo + i2, h2 = hk * a.group + (row0 + r2) % a.group;
+      const int r2 = warp * 4 + z + 16 * i, i2 = (row0 + r2) / a.group;
+      if (!paged_hidden_odd<DH / 32, float>(a, r.b, hk, DH, 0, max(t0 * XK, r.limit(i2, 1)), min(t1 * XK, n_keys))) continue;
+      const int tok2 = r.lo + i2, h2 = hk * a.group + (row0 + r2) % a.group;
       float o[DH / 32], M, sum;
       paged_row_alone<DH>(a, r.b, (const float*)a.q + tok2 * a.q_stride + (long long)h2 * DH, hk, t0 * XK, min(t1 * XK, r.limit(i2, 1)), o, M, sum);
       const size_t slot2 = ((size_t)range * a.pb.tokens + tok2) * a.hq + h2;
@@ -463,23 +464,35 @@ phyai_status_t bad_arg(const char* m) {
 
 // What a call launches: the kernel's row tile, its units and key ranges.
 struct Plan {
-  int f32, rt, units, ranges;
+  int f32, pair, rt, ranges;
+  long long units;
 };
 Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int max_pages, int n_sm) {
   Plan p{};
   const int group = hq / (int)c->n_kv_heads, holders = tokens < batch ? tokens : batch;      // requests with tokens, at most
   const long long rows = (long long)tokens * group;
   p.f32 = c->dtype == PHYAI_F32;
+  const long long keys = (long long)max_pages * c->page_size;
+  // More than 16 packed rows a request: the tensor cores' kernel, whose tiles of 256 rows cost what a tile's keys cost to fetch.
+  if (!p.f32 && rows > 16ll * holders && paged_pair_supported((int)c->head_dim, group)) {
+    const int per = paged_pair_tokens(group), pairs = paged_pair_resident((int)c->head_dim);
+    const long long full = (tokens + per - 1) / per > holders ? (tokens + per - 1) / per : holders;
+    p.pair = 1, p.units = tokens / per + holders;
+    // key ranges: a pair for each, of at least 256 keys
+    long long ranges = pairs / (full * c->n_kv_heads);
+    if (ranges > keys / 256) ranges = keys / 256;
+    p.ranges = (int)(ranges < 1 ? 1 : ranges > 64 ? 64 : ranges);
+    return p;
+  }
   if (p.f32) {
     p.rt = rows > 16ll * holders ? 64 : 16;
   } else {
     const int most = c->head_dim == 64 ? 32 : 16;
     p.rt = rows <= 8ll * holders ? 8 : rows <= 16ll * holders || most == 16 ? 16 : most;
   }
-  p.units = (int)(rows / p.rt) + holders;
+  p.units = rows / p.rt + holders;
   // key ranges: enough blocks for two rounds of the SMs, of at least 128 keys
   const long long full = (rows + p.rt - 1) / p.rt > holders ? (rows + p.rt - 1) / p.rt : holders, blocks = full * c->n_kv_heads;
-  const long long keys = (long long)max_pages * c->page_size;
   long long ranges = (2ll * n_sm + blocks - 1) / blocks;
   if (ranges > keys / 128) ranges = keys / 128;
   p.ranges = (int)(ranges < 1 ? 1 : ranges > 64 ? 64 : ranges);
@@ -500,7 +513,7 @@ cudaError_t launch_few(const PagedAttn& a, const Plan& p, const CUtensorMap& map
     if (e != cudaSuccess) return e;
     once.done();
   }
-  return launch_pdl(k_paged_few<DH, NT>, dim3(p.units, a.hkv, p.ranges), dim3(FW * 32), Few<DH>::SMEM, st, a, map);
+  return launch_pdl(k_paged_few<DH, NT>, dim3((unsigned)p.units, a.hkv, p.ranges), dim3(FW * 32), Few<DH>::SMEM, st, a, map);
 }
 template <int DH, int RR>
 cudaError_t launch_f32(const PagedAttn& a, const Plan& p, cudaStream_t st) {
@@ -511,20 +524,20 @@ cudaError_t launch_f32(const PagedAttn& a, const Plan& p, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     once.done();
   }
-  return launch_pdl(k_paged_f32<DH, RR>, dim3(p.units, a.hkv, p.ranges), dim3(XT), smem, st, a);
+  return launch_pdl(k_paged_f32<DH, RR>, dim3((unsigned)p.units, a.hkv, p.ranges), dim3(XT), smem, st, a);
 }
-// the pool as rows of 64 channels: {64, rows of a plane, blocks of 64 channels in a row, planes}, copies of `box` rows of a head
-bool pool_map(CUtensorMap* m, const phyai_paged_cache_t* c, uint32_t box) {
+}  // namespace
+
+bool paged_pool_map(void* map, const phyai_paged_cache_t* c, uint32_t rows, uint32_t blocks) {
   const EncodeTiled enc = encode_tiled();
   if (!enc) return false;
-  const cuuint64_t row = (cuuint64_t)c->n_kv_heads * c->head_dim * 2, rows = c->n_pages * c->page_size;
-  const cuuint64_t dims[4] = {64, rows, row / 128, 2ull * c->n_layers}, strides[3] = {row, 128, rows * row};
-  const cuuint32_t bx[4] = {64, box, c->head_dim / 64, 1}, es[4] = {1, 1, 1, 1};
-  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, c->pages, dims, strides, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t row = (cuuint64_t)c->n_kv_heads * c->head_dim * 2, n = c->n_pages * c->page_size;
+  const cuuint64_t dims[4] = {64, n, row / 128, 2ull * c->n_layers}, strides[3] = {row, 128, n * row};
+  const cuuint32_t bx[4] = {64, rows, blocks, 1}, es[4] = {1, 1, 1, 1};
+  return enc(reinterpret_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, c->pages, dims, strides, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-}  // namespace
 }  // namespace phyai
 
 extern "C" {
@@ -580,9 +593,11 @@ phyai_status_t phyai_paged_attention(const phyai_paged_cache_t* cache, uint32_t 
     if (dh == 64) e = p.rt == 16 ? launch_f32<64, 1>(a, p, st) : launch_f32<64, 4>(a, p, st);
     else if (dh == 128) e = p.rt == 16 ? launch_f32<128, 1>(a, p, st) : launch_f32<128, 4>(a, p, st);
     else e = p.rt == 16 ? launch_f32<256, 1>(a, p, st) : launch_f32<256, 4>(a, p, st);
+  } else if (p.pair) {
+    e = launch_paged_pair(a, cache, p.units * a.hkv * p.ranges, st);
   } else {
     CUtensorMap map;
-    if (!pool_map(&map, cache, 16)) {
+    if (!paged_pool_map(&map, cache, 16, cache->head_dim / 64)) {
       snprintf(g_paged_err, sizeof(g_paged_err), "cuTensorMapEncodeTiled failed");
       return PHYAI_ERR_CUDA;
     }

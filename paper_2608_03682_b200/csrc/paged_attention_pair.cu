@@ -1,0 +1,533 @@
+// Attention of many new tokens over a paged cache: a persistent grid of CTA pairs (tcgen05 cta_group::2).
+//
+// A pair takes a unit: 2 x 128 packed rows (each CTA floor(128 / group) tokens of a request with the query heads of one kv head) and
+// walks the keys that any of them sees, then goes on to its next unit without leaving the pipeline: the next unit's operands are on their way
+// and its first logits go through the softmax while the accumulator of the last one is read out.
+//   S = Q K^T   M = 256, N = 128 keys, K = head_dim; Q and K in shared memory; two S buffers in tensor memory
+//   softmax     two threads per row (half of the columns each), straight from tensor memory; P (bf16) over the S buffer; the accumulator
+//               is rescaled only when a maximum grows by more than 2^8 (the old one is kept otherwise: exact algebra)
+//   O += P V    M = 256, N = head_dim, K = 128 keys; P is the tensor-memory A operand, V an MN-major B operand
+// K: CTA h of the pair fetches block h (64 keys) of a tile, V: its half of the channels of both blocks; the tensor cores read the other
+// half from the peer, so that every SM fetches and reads half of a tile: with one CTA per 128 rows the shared memory (Q 128 + K 128 rows
+// per product, at 128 bytes a clock) would bound the products.  All operands come by tensor-map copies, keys and values piece by piece:
+// a piece is the rows of a page, 64 at most, one lane of the loading warp per copy.  Rows past the cached tokens may hold anything: their
+// logits are masked by index, their values overwritten with zeros in shared memory (0 x NaN); pieces of pages that a request does not have
+// are fetched from past the pool, which fills in zeros.  Keys inside a tile that a row does not see (causal) may hold infinities, too:
+// rows whose result is not finite are looked at again after the last unit (see paged_row_alone).
+//
+// Few units (short chunks over long histories): a unit's keys are split over several pairs, the fp32 results are merged by k_paged_merge.
+// Warps of a CTA: 0 fetches K, 1 V, 2 Q, 3 issues the MMAs (leader CTA), 4-11 softmax, correction, output.  Every wait is bounded; after
+// a give-up the protocol runs to its end and only the global stores are skipped.
+#include <cstdio>
+
+#include "paged.cuh"
+#include "attention.cuh"
+#include "attention_choice.h"
+#include "tc_pair.cuh"
+
+namespace phyai {
+namespace {
+
+constexpr int KB = 128;                        // keys per tile: two blocks of 64
+constexpr int PP_THREADS = 12 * 32;
+constexpr int PAIR_LEAST = 2;                  // tiles of keys in a range, at least
+
+template <int DH>
+struct PpLayout {
+  static constexpr int KBLOCK = 64 * 128;                    // 64 channels of 64 keys
+  static constexpr int PIECE = (DH / 128) * KBLOCK;          // 64 keys x DH / 2 channels
+  static constexpr int TILE = 2 * PIECE;                     // K: this CTA's block; V: both blocks, its channel half
+  static constexpr int QTILE = 128 * DH * 2;
+  static constexpr int STG = 2048;                           // output staging of a warp: 32 rows x 32 columns
+  static constexpr size_t SMEM = 1024 + 4 * (size_t)TILE + QTILE + 8 * STG;
+};
+
+__device__ __forceinline__ void copy4d(uint32_t dst, const CUtensorMap* map, int c1, int c2, int c3, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+      : "memory");
+}
+
+struct Unit {
+  PagedRequest r;      // r.b < 0: none
+  int hk, tok0;        // first of the unit's tokens in the request
+  int t0, T;           // tiles of 128 keys: first, how many (one at least: without a key all of it is masked)
+  int range, ranges;
+  int index;           // of the call's units x kv heads x ranges
+};
+
+template <int DH>
+__global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
+    k_paged_pair(const PagedAttn a, const __grid_constant__ CUtensorMap tmq, const __grid_constant__ CUtensorMap tmkv, const int piece_shift) {
+  using L = PpLayout<DH>;
+  constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(KB >> 3) << 17) | ((256u >> 4) << 24);
+  constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((256u >> 4) << 24);
+
+  extern __shared__ uint8_t smem_raw[];
+  // leader: operands of a buffer complete in both CTAs, P of a buffer (by column half) complete in both, Q complete in both, accumulator
+  // read out in both.  Each CTA: logits / P V complete, all logits of a unit complete; own V blocks that are cleared in part.
+  __shared__ __align__(8) uint64_t k_full[2], v_full[2], p_full[2][2], q_full, o_free, s_full[2], pv_done[2], q_free, v_own;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag, s_skip;
+  __shared__ float xch[2][2][128], xsum[2][2][128];       // what the two half-row threads of a row exchange: maximum (by tile parity), sum (by unit parity)
+  __shared__ int s_first[PAGED_MAX_BATCH + 1], s_warp[PP_THREADS / 32];
+
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const int half = blockIdx.x & 1, pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const int G = a.group, TOK = 128 / G;                   // tokens of a CTA's 128 rows
+  if (tid == 32) prefetch_tmap(&tmkv), prefetch_tmap(&tmq);
+
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t Ks = base, Vs = base + 2 * L::TILE, Qs = base + 4 * L::TILE;
+  if (tid == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&k_full[i]), 1), mbar_init(smem_u32(&v_full[i]), 2), mbar_init(smem_u32(&p_full[i][0]), 8), mbar_init(smem_u32(&p_full[i][1]), 8);
+      mbar_init(smem_u32(&s_full[i]), 1), mbar_init(smem_u32(&pv_done[i]), 1);
+    }
+    mbar_init(smem_u32(&q_full), 1), mbar_init(smem_u32(&o_free), 16), mbar_init(smem_u32(&q_free), 1), mbar_init(smem_u32(&v_own), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 3) {
+    tmem_alloc2(smem_u32(&tmem_slot), 512);
+    tc_fence_before();
+  }
+  __syncthreads();
+  pair_sync();                                      // both CTAs' barriers exist before the peer can signal them
+  tc_fence_after();
+  pdl_launch_dependents();                          // (not before: a later kernel must not take tensor memory that this one still waits for)
+  const uint32_t tmem_base = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&tmem_slot), 0);
+  const uint32_t tmem_s = tmem_base, tmem_o = tmem_base + 2 * KB;
+  const WaitCtx wc{a.status, &abort_flag, a.wait_limit}, wl{a.status, &abort_flag, a.wait_limit, true};
+
+  // ---- units before each request (both CTAs of a pair read the same lengths and come to the same list)
+  pdl_wait();
+  if (tid == 0) s_skip = status_set(a.status), s_first[0] = 0;
+  bool bad = false;
+  int acc = 0;
+  for (int i0 = 0; i0 < a.pb.batch; i0 += PP_THREADS) {
+    const int i = i0 + tid;
+    int n = 0;
+    if (i < a.pb.batch) {
+      const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1];
+      const bool b = paged_entry_bad(a.pb, i, lo, hi, a.pb.kv_lens[i], false);
+      bad |= b;
+      n = b ? 0 : (hi - lo + 2 * TOK - 1) / (2 * TOK);
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, n, o);
+      if (lane >= o) n += up;
+    }
+    if (lane == 31) s_warp[warp] = n;
+    __syncthreads();
+    int before = acc;
+    for (int w = 0; w < PP_THREADS / 32; ++w) {
+      if (w < warp) before += s_warp[w];
+      acc += s_warp[w];
+    }
+    if (i < a.pb.batch) s_first[i + 1] = before + n;
+    __syncthreads();
+  }
+  bad = __syncthreads_or(bad);
+  if (bad && tid == 0) atomicExch(a.status, ST_INVALID_ARG);
+  const bool skip = s_skip != 0;
+  const int n_units = bad ? 0 : acc * a.hkv * a.ranges;
+
+  // Units of this pair: of every round of n_pairs units one, rounds dealt back and forth (a request's last, longest tiles come first).
+  auto index_of = [&](int k) { return k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair); };
+  auto unit_at = [&](int j) {
+    Unit u;
+    u.index = j, u.range = a.ranges > 1 ? j % a.ranges : 0;
+    const int uh = a.ranges > 1 ? j / a.ranges : j, ut = a.hkv > 1 ? uh / a.hkv : uh;
+    u.hk = uh - ut * a.hkv;
+    int lo = 0, hi = a.pb.batch;                    // s_first[lo] <= ut < s_first[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (s_first[mid] <= ut) lo = mid;
+      else hi = mid;
+    }
+    u.r.b = lo, u.r.lo = a.pb.cu[lo], u.r.n = a.pb.cu[lo + 1] - u.r.lo, u.r.kv = a.pb.kv_lens[lo];
+    u.r.prefix = a.prefix_lens ? min(max(a.prefix_lens[lo], 0), u.r.kv) : 0;
+    u.tok0 = (s_first[lo + 1] - 1 - ut) * 2 * TOK;
+    const int keys = u.r.limit(min(u.tok0 + 2 * TOK, u.r.n) - 1, a.causal), tiles = max(1, (keys + KB - 1) / KB);
+    u.ranges = ranges_of(tiles, a.ranges, PAIR_LEAST);
+    u.t0 = u.range < u.ranges ? (int)((long long)tiles * u.range / u.ranges) : 0;
+    u.T = u.range < u.ranges ? (int)((long long)tiles * (u.range + 1) / u.ranges) - u.t0 : 0;
+    return u;
+  };
+  // the first unit of this pair from its round k on; k moves past it
+  auto next_unit = [&](int& k) {
+    for (int j; (j = index_of(k)) < n_units || k * n_pairs < n_units;) {
+      ++k;
+      if (j >= n_units) continue;
+      const Unit u = unit_at(j);
+      if (u.T > 0) return u;
+    }
+    Unit u{};
+    u.r.b = -1, u.T = 0;
+    return u;
+  };
+  // row of the planes of key `key` of a unit's request; past the pool where the request has no page for it (or a wrong entry)
+  const int past = a.pb.n_pages << a.pb.page_shift;
+  auto row_of = [&](const PagedRequest& r, int key) {
+    if (key >= r.kv) return past;
+    const int page = a.pb.table[(size_t)r.b * a.pb.max_pages + (key >> a.pb.page_shift)];
+    if ((unsigned)page >= (unsigned)a.pb.n_pages) {
+      atomicExch(a.status, ST_INVALID_ARG);
+      return past;
+    }
+    return (page << a.pb.page_shift) + (key & ((1 << a.pb.page_shift) - 1));
+  };
+  const int np = 64 >> piece_shift;                 // pieces of a block of 64 keys
+  const int cb = np == 1 ? DH / 128 : 1;            // blocks of 64 channels of a copy
+  const uint32_t piece_bytes = (uint32_t)(128 << piece_shift);
+
+  if (warp == 0) {
+    // =========================== K: a buffer is free again once the logits of the tile two before exist ==================
+    const int nc = np * (DH / 64 / cb), pc = lane % np, ch = (lane / np) * cb;        // copies of a block: one per lane
+    int k = 0, n = 0;
+    Unit u = next_unit(k);
+    while (u.r.b >= 0) {
+      for (int t = 0; t < u.T; ++t, ++n) {
+        const int row = lane < nc ? row_of(u.r, (u.t0 + t) * KB + half * 64 + (pc << piece_shift)) : 0;
+        if (n >= 2 && lane == 0) mbar_wait_drain(smem_u32(&s_full[n & 1]), (uint32_t)((n - 2) >> 1) & 1u, wl);
+        __syncwarp();
+        const uint32_t bar = smem_u32(&k_full[n & 1]), dst = Ks + (uint32_t)(n & 1) * L::TILE;
+        if (half == 0 && lane == 0) mbar_expect_tx(bar, (uint32_t)L::TILE * 2);
+        __syncwarp();
+        if (lane < nc) copy4d(dst + (uint32_t)ch * L::KBLOCK + (uint32_t)pc * piece_bytes, &tmkv, row, u.hk * (DH / 64) + ch, a.plane, bar & LEADER_MASK);
+      }
+      u = next_unit(k);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // =========================== V: a buffer is free again once P V of the tile two before has completed ==================
+    const uint32_t full_lead = map_rank(smem_u32(&v_full[0]), 0);
+    const int nb = np * (DH / 128 / cb), blk = lane / nb, pc = lane % np, ch = ((lane % nb) / np) * cb;   // copies of a block; block of this lane
+    uint32_t ph_own = 0;
+    int k = 0, n = 0;
+    Unit u = next_unit(k);
+    while (u.r.b >= 0) {
+      for (int t = 0; t < u.T; ++t, ++n) {
+        const int key0 = (u.t0 + t) * KB, rem = u.r.kv - key0;                        // rows past the cached tokens: rem .. of the tile
+        // (rows up to the end of the piece that they begin in; later pieces are zeros)
+        const int clear_to = (rem + (1 << piece_shift) - 1) >> piece_shift << piece_shift;
+        const bool clear = rem > 0 && rem < KB && clear_to > rem;
+        const int row = lane < 2 * nb ? row_of(u.r, key0 + blk * 64 + (pc << piece_shift)) : 0;
+        const uint32_t dst = Vs + (uint32_t)(n & 1) * L::TILE;
+        uint32_t bar = smem_u32(&v_full[n & 1]);
+        if (lane == 0) {
+          if (n >= 2) mbar_wait_drain(smem_u32(&pv_done[n & 1]), (uint32_t)((n - 2) >> 1) & 1u, wl);
+          if (clear) mbar_expect_tx(smem_u32(&v_own), (uint32_t)L::TILE);
+          else if (half == 0) mbar_expect_tx(bar, 2 * (uint32_t)L::TILE);
+          else remote_arrive(full_lead + (uint32_t)(n & 1) * 8u);
+        }
+        __syncwarp();
+        bar = clear ? smem_u32(&v_own) : bar & LEADER_MASK;
+        if (lane < 2 * nb)
+          copy4d(dst + (uint32_t)blk * L::PIECE + (uint32_t)ch * L::KBLOCK + (uint32_t)pc * piece_bytes, &tmkv, row, u.hk * (DH / 64) + half * (DH / 128) + ch,
+                 a.plane + 1, bar);
+        if (clear) {
+          mbar_wait_drain(bar, ph_own, wl);
+          ph_own ^= 1u;
+          for (int i = lane; i < (clear_to - rem) * (DH / 16); i += 32) {              // (a row: 8 x 16 bytes in each of DH / 128 blocks)
+            const int r = rem + i / (DH / 16), c = i % (DH / 16);
+            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(dst + (uint32_t)((r >> 6) * L::PIECE + (c >> 3) * L::KBLOCK + (r & 63) * 128 + (c & 7) * 16)), "r"(0u) : "memory");
+          }
+          fence_async_smem();                    // generic-proxy writes, read next by the tensor cores
+          __syncwarp();
+          if (lane == 0) remote_arrive_stores(full_lead + (uint32_t)(n & 1) * 8u);
+        }
+      }
+      u = next_unit(k);
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    // =========================== Q: its tile is free again once the last logits of the unit before exist ==================
+    if (lane == 0) {
+      int k = 0, i = 0;
+      for (Unit u = next_unit(k); u.r.b >= 0; u = next_unit(k), ++i) {
+        if (i > 0) mbar_wait_drain(smem_u32(&q_free), (uint32_t)(i - 1) & 1u, wl);
+        const uint32_t bar = smem_u32(&q_full);
+        if (half == 0) mbar_expect_tx(bar, 2 * (uint32_t)(TOK * G * DH * 2));
+#pragma unroll
+        for (int c = 0; c < DH / 64; ++c) copy4d(Qs + (uint32_t)c * (128 * 128), &tmq, u.hk * G, u.r.lo + u.tok0 + half * TOK, c, bar & LEADER_MASK);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 3) {
+    // =========================== MMA issuer (leader CTA): S(0), S(1), then P(n) V(n), S(n + 2), across the units ==========
+    if (half == 0) {
+      // S(n) may be issued once P V of tile n - 2 has been (its S buffer holds P of that tile).  Of the next logits and the next
+      // P V whichever has its operands goes first; logits when both have.
+      int k_s = 0, k_p = 0, ns = 0, is = 0, ts = 0, np_ = 0, ip = 0, tp = 0;      // tile of the call, unit, tile of the unit: of logits, of P V
+      Unit us = next_unit(k_s), up = us;
+      k_p = k_s;
+      uint32_t spins = 0;
+      while (up.r.b >= 0) {
+        if (us.r.b >= 0 && ns < np_ + 2) {
+          bool go = mbar_test(smem_u32(&k_full[ns & 1]), (uint32_t)(ns >> 1) & 1u) && (ts > 0 || mbar_test(smem_u32(&q_full), (uint32_t)is & 1u));
+          if (spins >= a.wait_limit) {             // given up: the protocol goes on in a fixed order
+            mbar_wait_drain(smem_u32(&k_full[ns & 1]), (uint32_t)(ns >> 1) & 1u, wc);
+            if (ts == 0) mbar_wait_drain(smem_u32(&q_full), (uint32_t)is & 1u, wc);
+            go = true;
+          }
+          if (__all_sync(0xffffffffu, go)) {
+            tc_fence_after();
+            const uint32_t kb = Ks + (uint32_t)(ns & 1) * L::TILE;
+            uint64_t da = make_desc(Qs), db = make_desc(kb);      // (a 64-channel block further: 128 x 128 and 64 x 128 bytes)
+#pragma unroll 1
+            for (int c = 0; c < DH / 64; ++c, da += (128 * 128) >> 4, db += L::KBLOCK >> 4) {
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk)
+                if (elect_one()) umma2_bf16(tmem_s + (uint32_t)(ns & 1) * KB, da + 2 * kk, db + 2 * kk, IDESC_S, (c > 0 || kk > 0) ? 1u : 0u);
+            }
+            if (elect_one()) umma2_commit(smem_u32(&s_full[ns & 1]));
+            if (ts + 1 == us.T && elect_one()) umma2_commit(smem_u32(&q_free));
+            __syncwarp();
+            ++ns;
+            if (++ts == us.T) ts = 0, ++is, us = next_unit(k_s);
+            if (spins < a.wait_limit) spins = 0;
+            continue;
+          }
+        }
+        if (np_ < ns) {
+          const uint32_t pf = smem_u32(&p_full[np_ & 1][0]), par = (uint32_t)(np_ >> 1) & 1u;
+          bool go = mbar_test(smem_u32(&v_full[np_ & 1]), par) && mbar_test(pf, par) && (tp > 0 || ip == 0 || mbar_test(smem_u32(&o_free), (uint32_t)(ip - 1) & 1u));
+          if (spins >= a.wait_limit) {
+            mbar_wait_drain(smem_u32(&v_full[np_ & 1]), par, wc);
+            mbar_wait_drain(pf, par, wc);
+            if (tp == 0 && ip > 0) mbar_wait_drain(smem_u32(&o_free), (uint32_t)(ip - 1) & 1u, wc);
+            go = true;
+          }
+          if (__all_sync(0xffffffffu, go)) {
+            // (the tile in which the cached tokens end: rows of it were cleared by a warp of each CTA)
+            if (up.r.kv < (up.t0 + tp + 1) * KB) pair_acquire(smem_u32(&v_full[np_ & 1]), par);
+            const uint32_t vb = Vs + (uint32_t)(np_ & 1) * L::TILE;
+#pragma unroll 1
+            for (int kh = 0; kh < 2; ++kh) {
+              if (kh == 1) mbar_wait_drain(pf + 8u, par, wc);
+              tc_fence_after();
+              // A = P of this tile: bf16 pairs in the first 64 columns of its S buffer
+              const uint64_t db = make_desc_mn(vb + (uint32_t)kh * L::PIECE, L::KBLOCK, 1024);
+              const uint32_t tp_ = tmem_s + (uint32_t)(np_ & 1) * KB + (uint32_t)kh * 32;
+#pragma unroll
+              for (int kj = 0; kj < KB / 32; ++kj)
+                if (elect_one()) umma2_ts(tmem_o, tp_ + (uint32_t)kj * 8, db + kj * ((16 * 128) >> 4), IDESC_PV, (tp > 0 || kh > 0 || kj > 0) ? 1u : 0u);
+            }
+            if (elect_one()) umma2_commit(smem_u32(&pv_done[np_ & 1]));
+            __syncwarp();
+            ++np_;
+            if (++tp == up.T) tp = 0, ++ip, up = next_unit(k_p);
+            if (spins < a.wait_limit) spins = 0;
+            continue;
+          }
+        }
+        ++spins;
+      }
+    }
+    __syncwarp();
+  } else {
+    // =========================== softmax / correction / output ==============================================================
+    const int g = (warp - 4) >> 2;            // which half of a row's columns: block g of a tile
+    const int q = warp & 3;
+    const int row = q * 32 + lane;            // accumulator row = tensor-memory lane
+    const int row_tok = row / G;              // token of the CTA's TOK (rows past TOK * G: none)
+    const uint32_t lane_addr = (uint32_t)(q * 32) << 16;
+    const uint32_t pfull0 = map_rank(smem_u32(&p_full[0][g]), 0), ofree0 = map_rank(smem_u32(&o_free), 0);
+    const uint32_t ostage = Qs + L::QTILE + (uint32_t)(warp - 4) * L::STG;
+    const int c0 = g * (DH / 2);              // first of this warp's output channels
+    float m = -INFINITY, l = 0.f, m_prev = 0.f, l_prev = 0.f;             // running maximum (log2 units) and sum (of this thread's columns)
+    bool odd = false;
+    int k = 0, n = 0, i = 0;
+    Unit u = next_unit(k), prev = u;
+    int t = 0;
+    for (;;) {
+      if (u.r.b >= 0) {
+        const uint32_t sb = tmem_s + (uint32_t)(n & 1) * KB + lane_addr;
+        const int tok = u.tok0 + half * TOK + row_tok;
+        const int lim = row < TOK * G && tok < u.r.n ? u.r.limit(tok, a.causal) : 0;
+        const uint64_t vis = first_columns(lim - ((u.t0 + t) * KB + g * 64));
+        if (lane == 0) mbar_wait_drain(smem_u32(&s_full[n & 1]), (uint32_t)(n >> 1) & 1u, wc);
+        __syncwarp();
+        tc_fence_after();
+        pair_softmax_tile<DH>(m, l, xch[n & 1], sb, tmem_o + lane_addr, g, q, row, vis, true, [&] {
+          if (lane == 0) mbar_wait_drain(smem_u32(&pv_done[(n - 1) & 1]), (uint32_t)((n - 1) >> 1) & 1u, wc);
+        }, a.scale_log2);
+        if (lane == 0) remote_arrive(pfull0 + (uint32_t)(n & 1) * 16u);
+      }
+      if (t == 0 && i > 0) {
+        // ---- the unit before: O / l -> bf16, 32 columns at a time through a staging block of the warp, out with coalesced stores; or the
+        // accumulator of a key range as it is
+        xsum[i & 1][g][row] = l_prev;
+        quarter_sync(q);
+        const float sum = xsum[i & 1][0][row] + xsum[i & 1][1][row];
+        const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+        if (lane == 0) mbar_wait_drain(smem_u32(&pv_done[(n - 1) & 1]), (uint32_t)((n - 1) >> 1) & 1u, wc);
+        __syncwarp();
+        tc_fence_after();
+        const bool okf = !skip && !*reinterpret_cast<volatile int*>(&abort_flag);
+        const int first_tok = prev.r.lo + prev.tok0 + half * TOK, n_rows = okf ? min(TOK, prev.r.n - prev.tok0 - half * TOK) * G : 0;
+        const bool whole = prev.ranges == 1;
+        const size_t slot = ((size_t)prev.range * a.pb.tokens + first_tok + row_tok) * a.hq + prev.hk * G + (row - row_tok * G);
+        if (g == 0 && a.ranges > 1 && row < n_rows) a.part_ml[slot] = make_float4(m_prev, sum, (float)prev.ranges, 0.f);
+        const uint32_t rowp = ostage + (uint32_t)lane * 64u;
+#pragma unroll 1
+        for (int c = 0; c < DH / 2; c += 32) {
+          float o[32];
+          tmem_ld32(tmem_o + lane_addr + (uint32_t)(c0 + c), o);
+          if (c + 32 == DH / 2) {                   // the accumulator may be overwritten
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) remote_arrive(ofree0);
+          }
+          float fin = 0.f;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) fin += fabsf(o[e]);
+          odd |= row < n_rows && !(fin < INFINITY);
+          if (!whole) {
+            if (row < n_rows) {
+              float* p = a.part_o + slot * DH + c0 + c;
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            }
+            continue;
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 8)
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(rowp + (uint32_t)(((e >> 3) ^ ((lane >> 1) & 3)) << 4)),
+                         "r"(pack_bf16(o[e] * inv, o[e + 1] * inv)), "r"(pack_bf16(o[e + 2] * inv, o[e + 3] * inv)),
+                         "r"(pack_bf16(o[e + 4] * inv, o[e + 5] * inv)), "r"(pack_bf16(o[e + 6] * inv, o[e + 7] * inv))
+                         : "memory");
+          __syncwarp();
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int rr = (lane >> 2) + 8 * x, ch = lane & 3, r = q * 32 + rr;
+            uint4 v;
+            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                         : "r"(ostage + (uint32_t)(rr * 64 + ((ch ^ ((rr >> 1) & 3)) << 4))) : "memory");
+            if (r < n_rows) {
+              const int rt = r / G;
+              *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + ((size_t)(first_tok + rt) * a.hq + prev.hk * G + (r - rt * G)) * DH + c0 + c + ch * 8) = v;
+            }
+          }
+          __syncwarp();
+        }
+      }
+      if (u.r.b < 0) break;
+      ++n;
+      if (++t == u.T) {
+        l_prev = l, m_prev = m, m = -INFINITY, l = 0.f;
+        prev = u, t = 0, ++i, u = next_unit(k);
+      }
+    }
+    // ---- rows that are not finite although the values that they see may be: those of them with an infinity or a NaN among the keys of
+    // their tiles that they do not see once more, key by key (channel by channel right otherwise: an infinite value is of one channel)
+    if (a.causal) {
+      __threadfence();
+      quarter_sync(q);                      // (maxima beside a range's result: written by the other warp of the quarter)
+    }
+    if (a.causal && __any_sync(0xffffffffu, odd) && !*reinterpret_cast<volatile int*>(&abort_flag)) {
+      k = 0;
+      for (u = next_unit(k); u.r.b >= 0; u = next_unit(k)) {
+        const int n_rows = min(TOK, u.r.n - u.tok0 - half * TOK) * G, end = min((u.t0 + u.T) * KB, u.r.kv);
+        for (int rr = q * 32; rr < min(n_rows, q * 32 + 32); ++rr) {
+          constexpr int C = DH / 64;
+          const int rt = rr / G, tok = u.r.lo + u.tok0 + half * TOK + rt, head = u.hk * G + rr - rt * G;
+          const int lim = u.r.limit(u.tok0 + half * TOK + rt, 1);
+          const size_t slot = ((size_t)u.range * a.pb.tokens + tok) * a.hq + head;
+          __nv_bfloat16* ob = (__nv_bfloat16*)a.out + ((size_t)tok * a.hq + head) * DH + c0;
+          float* of = a.part_o + slot * DH + c0;
+          bool bad_row = false;
+          for (int e = 0; e < C; ++e) bad_row |= !(fabsf(u.ranges == 1 ? __bfloat162float(ob[lane * C + e]) : of[lane * C + e]) < INFINITY);
+          if (!__any_sync(0xffffffffu, bad_row)) continue;
+          if (!paged_hidden_odd<C, __nv_bfloat16>(a, u.r.b, u.hk, DH, c0, max(u.t0 * KB, lim), end)) continue;
+          float o[DH / 32], M, sum;
+          paged_row_alone<DH>(a, u.r.b, (const __nv_bfloat16*)a.q + tok * a.q_stride + (long long)head * DH, u.hk, u.t0 * KB, min(end, lim), o, M, sum);
+          // (a key range's result is relative to the maximum that stands beside it)
+          const float w = u.ranges == 1 ? (sum > 0.f || sum != sum ? 1.0f / sum : 0.f) : M == -INFINITY ? 0.f : exp2f(M - a.part_ml[slot].x);
+#pragma unroll
+          for (int e = 0; e < DH / 32; ++e) {
+            const int c = lane * (DH / 32) + e - c0;
+            if (c < 0 || c >= DH / 2) continue;
+            if (u.ranges == 1) ob[c] = __float2bfloat16_rn(o[e] * w);
+            else of[c] = o[e] * w;
+          }
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  // Neither CTA leaves (or gives its tensor memory back) while the other still works: the leader's MMAs read both CTAs'
+  // shared memory and write both tensor memories.
+  cluster_arrive_relaxed();
+  cluster_wait();
+  if (warp == 3) {
+    tc_fence_after();
+    tmem_dealloc2(tmem_base, 512);
+  }
+}
+
+// query rows: copies of 64 channels of `group` heads of 128 / group tokens
+bool query_map(CUtensorMap* m, const PagedAttn& a, int dh) {
+  const EncodeTiled enc = encode_tiled();
+  if (!enc) return false;
+  const cuuint64_t dims[4] = {64, (cuuint64_t)a.hq, (cuuint64_t)a.pb.tokens, (cuuint64_t)dh / 64};
+  const cuuint64_t strides[3] = {(cuuint64_t)dh * 2, (cuuint64_t)a.q_stride * 2, 128};
+  const cuuint32_t box[4] = {64, (cuuint32_t)a.group, (cuuint32_t)(128 / a.group), 1}, es[4] = {1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(a.q), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DH>
+cudaError_t setup_one() {
+  static PerDeviceOnce once;
+  if (!once.needed()) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(k_paged_pair<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PpLayout<DH>::SMEM);
+  if (e == cudaSuccess) once.done();
+  return e;
+}
+template <int DH>
+int resident_one() {
+  if (setup_one<DH>() != cudaSuccess) return 0;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(1024), cfg.blockDim = dim3(PP_THREADS), cfg.dynamicSmemBytes = PpLayout<DH>::SMEM;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 2, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+  cfg.attrs = at, cfg.numAttrs = 1;
+  int n = 0;
+  return cudaOccupancyMaxActiveClusters(&n, k_paged_pair<DH>, &cfg) == cudaSuccess ? n : 0;
+}
+
+template <int DH>
+cudaError_t launch_one(const PagedAttn& a, const phyai_paged_cache_t* cache, long long items, cudaStream_t st) {
+  cudaError_t e = setup_one<DH>();
+  if (e != cudaSuccess) return e;
+  const int pairs = paged_pair_resident(DH);
+  if (items < 1 || pairs < 1) return cudaErrorInvalidConfiguration;
+  const int piece_shift = a.pb.page_shift < 6 ? a.pb.page_shift : 6;
+  CUtensorMap tq, tkv;
+  if (!query_map(&tq, a, DH) || !paged_pool_map(&tkv, cache, 1u << piece_shift, piece_shift == 6 ? DH / 128 : 1)) return cudaErrorInvalidValue;
+  const unsigned grid = 2u * (unsigned)(items < pairs ? items : pairs);
+  return launch_pdl(k_paged_pair<DH>, dim3(grid), dim3(PP_THREADS), PpLayout<DH>::SMEM, st, a, tq, tkv, piece_shift);
+}
+
+}  // namespace
+
+bool paged_pair_supported(int dh, int group) { return (dh == 128 || dh == 256) && group <= 128 && paged_pair_resident(dh) > 0; }
+int paged_pair_tokens(int group) { return 2 * (128 / group); }
+
+int paged_pair_resident(int dh) {
+  static PerDeviceCount resident[2];
+  return dh == 256 ? resident[1].get(resident_one<256>) : resident[0].get(resident_one<128>);
+}
+
+cudaError_t launch_paged_pair(const PagedAttn& a, const phyai_paged_cache_t* cache, long long items, cudaStream_t st) {
+  return cache->head_dim == 256 ? launch_one<256>(a, cache, items, st) : launch_one<128>(a, cache, items, st);
+}
+
+}  // namespace phyai
