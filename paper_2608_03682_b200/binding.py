@@ -506,58 +506,85 @@ def w8a8_project(x: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
 _STORE = {torch.float32: DTYPES["f32"], torch.bfloat16: DTYPES["bf16"]}
 
 
-class _Launch:
-    """Device and stream of a call: the tensors' device becomes the current one, outputs are allocated on the call's stream."""
+class _Elsewhere:
+    """A call on a given stream or another device: the device becomes the current one, outputs are allocated on the call's stream."""
 
     def __init__(self, device: torch.device, stream):
-        self.device = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
-        self.stream = None if stream is None else torch.cuda.stream(stream)
-        self.raw = _raw_stream(stream, device) or None
+        self.device, self.stream, self.raw = torch.cuda.device(device), torch.cuda.stream(stream), _raw_stream(stream, device)
 
     def __enter__(self):
-        if self.device is not None:
-            self.device.__enter__()
-        if self.stream is not None:
-            self.stream.__enter__()
+        self.device.__enter__()
+        self.stream.__enter__()
         return self.raw
 
     def __exit__(self, *exc):
-        if self.stream is not None:
-            self.stream.__exit__(*exc)
-        if self.device is not None:
-            self.device.__exit__(*exc)
+        self.stream.__exit__(*exc)
+        self.device.__exit__(*exc)
 
 
-def _head_rows(name: str, t: torch.Tensor, device: torch.device, like: Optional[torch.Tensor] = None) -> int:
+class _Here:
+    """The usual call: current device, current stream."""
+
+    def __init__(self, index: int):
+        self.index = index
+
+    def __enter__(self):
+        return torch._C._cuda_getCurrentRawStream(self.index)
+
+    def __exit__(self, *exc):
+        pass
+
+
+_HERE_ON = [_Here(i) for i in range(64)]
+
+
+def _launch(device: torch.device, stream):
+    i = device.index
+    return _HERE_ON[i] if stream is None and i < 64 and i == torch._C._cuda_getDevice() else _Elsewhere(device, stream)
+
+
+def _head_rows(name: str, t: torch.Tensor, device: torch.device, dtype: Optional[torch.dtype] = None) -> int:
     """Checks rows of heads ``[T, heads, dh]`` (heads contiguous in a row); returns the row stride in elements."""
-    if t.dim() != 3 or t.dtype not in _STORE or t.device != device:
-        raise ValueError(f"{name} must be a float32 or bfloat16 tensor [tokens, heads, head_dim] on {device}")
+    if t.dim() != 3 or t.dtype not in _STORE or t.device != device or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be a {dtype or 'float32 or bfloat16'} tensor [tokens, heads, head_dim] on {device}")
     T, H, dh = t.shape
     row, head, one = t.stride()
-    if (dh > 1 and one != 1) or (H > 1 and head != dh):
+    if one != 1 or (head != dh and H > 1):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
-    if like is not None and (T != like.shape[0] or dh != like.shape[2] or t.dtype != like.dtype):
-        raise ValueError(f"{name} and the keys differ in tokens, head_dim or type")
     return row if T > 1 else H * dh
 
 
-def _ints(name: str, t: torch.Tensor, device: torch.device, *shape) -> int:
-    if t.dtype != torch.int32 or t.device != device or t.shape != shape or not t.is_contiguous():
+def _ints(name: str, t: torch.Tensor, device: torch.device, shape: tuple) -> int:
+    if t.dtype is not torch.int32 or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
     return t.data_ptr()
 
 
-def _floats(name: str, t: Optional[torch.Tensor], device: torch.device, *shape) -> Optional[int]:
-    if t is None:
-        return None
-    if t.dtype != torch.float32 or t.device != device or t.shape[-len(shape):] != shape or not t.is_contiguous():
+def _floats(name: str, t: torch.Tensor, device: torch.device, shape: tuple) -> int:
+    if t.dtype is not torch.float32 or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous float32 tensor {list(shape)} on {device}")
     return t.data_ptr()
 
 
-def _paged_check(lib, st: int):
-    if st != OK:
-        raise PhyaiError(st, lib.phyai_paged_last_error().decode())
+def _rope(t: torch.Tensor, device: torch.device, dh: int) -> int:
+    return _floats("rope_cos_sin", t, device, (t.shape[0], dh // 2, 2))
+
+
+_heads_descs: Dict[tuple, tuple] = {}     # sizes and types of a call's heads -> (descriptor, its address)
+
+
+def _heads_desc(*key) -> int:
+    d = _heads_descs.get(key)
+    if d is None:
+        if len(_heads_descs) >= 256:
+            _heads_descs.clear()
+        desc = HeadsDesc(C.sizeof(HeadsDesc), *key)
+        d = _heads_descs[key] = (desc, C.addressof(desc))
+    return d
+
+
+def _paged_fail(lib, st: int):
+    raise PhyaiError(st, lib.phyai_paged_last_error().decode())
 
 
 def norm_rope_heads(q: Optional[torch.Tensor], k: torch.Tensor, positions: Optional[torch.Tensor], rope_cos_sin: Optional[torch.Tensor],
@@ -569,24 +596,31 @@ def norm_rope_heads(q: Optional[torch.Tensor], k: torch.Tensor, positions: Optio
     lib = _lib or load_library()
     device = k.device
     k_row = _head_rows("k", k, device)
-    q_row = 0 if q is None else _head_rows("q", q, device, k)
     T, Hkv, dh = k.shape
-    Hq = 0 if q is None else q.shape[1]
+    Hq = q_row = 0
+    if q is not None:
+        q_row = _head_rows("q", q, device, k.dtype)
+        Tq, Hq, dq = q.shape
+        if Tq != T or dq != dh:
+            raise ValueError("q and k differ in tokens or head_dim")
     dtype = dtype or k.dtype
     if dtype not in _STORE:
         raise ValueError("dtype must be float32 or bfloat16")
-    desc = HeadsDesc(C.sizeof(HeadsDesc), Hq, Hkv, dh, _STORE[k.dtype], _STORE[dtype], eps)
-    rope, gq, gk = (_floats("rope_cos_sin", rope_cos_sin, device, dh // 2, 2), _floats("q_gain", q_gain, device, dh),
-                    _floats("k_gain", k_gain, device, dh))
-    pos = None if positions is None else _ints("positions", positions, device, T)
-    with _Launch(device, stream) as sp:
-        q_out = None if q is None else torch.empty(T, Hq, dh, dtype=dtype, device=device)
-        k_out = torch.empty(T, Hkv, dh, dtype=dtype, device=device)
+    desc = _heads_desc(Hq, Hkv, dh, _STORE[k.dtype], _STORE[dtype], eps)
+    rope = None if rope_cos_sin is None else _rope(rope_cos_sin, device, dh)
+    gq = None if q_gain is None else _floats("q_gain", q_gain, device, (dh,))
+    gk = None if k_gain is None else _floats("k_gain", k_gain, device, (dh,))
+    pos = None if positions is None else _ints("positions", positions, device, (T,))
+    with _launch(device, stream) as sp:
+        q_out = None if q is None else torch.empty((T, Hq, dh), dtype=dtype, device=device)
+        k_out = torch.empty((T, Hkv, dh), dtype=dtype, device=device)
         if status is None:
             status = torch.zeros(1, dtype=torch.int32, device=device)
-        _paged_check(lib, lib.phyai_norm_rope_heads(C.addressof(desc), T, _ptr(q), q_row, k.data_ptr(), k_row, pos, rope,
-                                                    0 if rope is None else rope_cos_sin.shape[0], gq, gk, _ptr(q_out), k_out.data_ptr(),
-                                                    _ints("status", status, device, 1), sp))
+        st = lib.phyai_norm_rope_heads(desc[1], T, None if q is None else q.data_ptr(), q_row, k.data_ptr(), k_row, pos, rope,
+                                       0 if rope is None else rope_cos_sin.shape[0], gq, gk, None if q is None else q_out.data_ptr(),
+                                       k_out.data_ptr(), _ints("status", status, device, (1,)), sp)
+    if st != OK:
+        _paged_fail(lib, st)
     return q_out, k_out
 
 
@@ -610,6 +644,7 @@ class PagedCache:
         self._desc_ptr = C.addressof(self._desc)
         self.status = torch.zeros(1, dtype=torch.int32, device=pages.device)
         self._status_ptr = self.status.data_ptr()
+        self._work: Dict[tuple, int] = {}     # sizes of a call -> bytes of its workspace
 
     def poll_status(self) -> int:
         """Read-and-clear the status word (synchronises); returns the status code."""
@@ -621,9 +656,10 @@ class PagedCache:
     def _requests(self, cu_q_lens, kv_lens, page_table):
         if page_table.dim() != 2:
             raise ValueError("page_table must be [batch, max_pages]")
-        B, most = page_table.shape
-        cu = None if cu_q_lens is None else _ints("cu_q_lens", cu_q_lens, self.device, B + 1)
-        return B, most, cu, _ints("kv_lens", kv_lens, self.device, B), _ints("page_table", page_table, self.device, B, most)
+        device = self.device
+        B, most = shape = page_table.shape
+        cu = None if cu_q_lens is None else _ints("cu_q_lens", cu_q_lens, device, (B + 1,))
+        return B, most, cu, _ints("kv_lens", kv_lens, device, (B,)), _ints("page_table", page_table, device, shape)
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, cu_q_lens: torch.Tensor, kv_lens: torch.Tensor, page_table: torch.Tensor,
                rope_cos_sin: Optional[torch.Tensor], k_gain: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
@@ -631,22 +667,29 @@ class PagedCache:
         """New keys (normed with gain ``1 + k_gain`` unless None, rotated) and values ``[T, Hkv, dh]`` into the pages of ``layer``; with
         ``q`` ``[T, Hq, dh]`` returns its normed, rotated rows in the cache's type (rows of no request are not written), else None."""
         lib, device = self.lib, self.device
-        k_row, v_row = _head_rows("k", k, device), _head_rows("v", v, device, k)
-        q_row = 0 if q is None else _head_rows("q", q, device, k)
+        k_row, v_row = _head_rows("k", k, device), _head_rows("v", v, device, k.dtype)
         T, Hkv, dh = k.shape
-        if v.shape[1] != Hkv:
-            raise ValueError("k and v differ in heads")
-        Hq = 0 if q is None else q.shape[1]
-        desc = HeadsDesc(C.sizeof(HeadsDesc), Hq, Hkv, dh, _STORE[k.dtype], _STORE[self.dtype], eps)
+        if v.shape != k.shape:
+            raise ValueError("k and v differ in tokens, heads or head_dim")
+        Hq = q_row = 0
+        if q is not None:
+            q_row = _head_rows("q", q, device, k.dtype)
+            Tq, Hq, dq = q.shape
+            if Tq != T or dq != dh:
+                raise ValueError("q and k differ in tokens or head_dim")
+        desc = _heads_desc(Hq, Hkv, dh, _STORE[k.dtype], self._desc.dtype, eps)
         B, most, cu, lens, table = self._requests(cu_q_lens, kv_lens, page_table)
-        rope, gq, gk = (_floats("rope_cos_sin", rope_cos_sin, device, dh // 2, 2), _floats("q_gain", q_gain, device, dh),
-                        _floats("k_gain", k_gain, device, dh))
-        pos = None if positions is None else _ints("positions", positions, device, T)
-        with _Launch(device, stream) as sp:
-            q_out = None if q is None else torch.empty(T, Hq, dh, dtype=self.dtype, device=device)
-            _paged_check(lib, lib.phyai_append_paged_kv(self._desc_ptr, C.addressof(desc), layer, T, _ptr(q), q_row, k.data_ptr(), k_row,
-                                                        v.data_ptr(), v_row, B, cu, lens, table, most, pos, rope,
-                                                        0 if rope is None else rope_cos_sin.shape[0], gq, gk, _ptr(q_out), self._status_ptr, sp))
+        rope = None if rope_cos_sin is None else _rope(rope_cos_sin, device, dh)
+        gq = None if q_gain is None else _floats("q_gain", q_gain, device, (dh,))
+        gk = None if k_gain is None else _floats("k_gain", k_gain, device, (dh,))
+        pos = None if positions is None else _ints("positions", positions, device, (T,))
+        with _launch(device, stream) as sp:
+            q_out = None if q is None else torch.empty((T, Hq, dh), dtype=self.dtype, device=device)
+            st = lib.phyai_append_paged_kv(self._desc_ptr, desc[1], layer, T, None if q is None else q.data_ptr(), q_row, k.data_ptr(), k_row,
+                                           v.data_ptr(), v_row, B, cu, lens, table, most, pos, rope, 0 if rope is None else rope_cos_sin.shape[0],
+                                           gq, gk, None if q is None else q_out.data_ptr(), self._status_ptr, sp)
+        if st != OK:
+            _paged_fail(lib, st)
         return q_out
 
     def attend(self, layer: int, q: torch.Tensor, cu_q_lens: torch.Tensor, kv_lens: torch.Tensor, page_table: torch.Tensor, causal: bool = True,
@@ -655,24 +698,30 @@ class PagedCache:
         included.  ``causal``: a token sees what is cached before it and itself, and with ``prefix_lens`` (int32 ``[B]``) the first so many
         tokens.  Returns ``out`` ``[T, Hq, dh]`` (rows of no request are not written)."""
         lib, device = self.lib, self.device
-        row = _head_rows("q", q, device)
-        T, Hq, dh = q.shape
-        if q.dtype != self.dtype or dh != self.head_dim:
-            raise ValueError("q and the cache differ in type or head_dim")
+        row = _head_rows("q", q, device, self.dtype)
+        T, Hq, dh = shape = q.shape
+        if dh != self.head_dim:
+            raise ValueError("q and the cache differ in head_dim")
         B, most, cu, lens, table = self._requests(cu_q_lens, kv_lens, page_table)
-        prefix = None if prefix_lens is None else _ints("prefix_lens", prefix_lens, device, B)
-        if out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != device or not out.is_contiguous()):
+        prefix = None if prefix_lens is None else _ints("prefix_lens", prefix_lens, device, (B,))
+        if out is not None and (out.shape != shape or out.dtype != q.dtype or out.device != device or not out.is_contiguous()):
             raise ValueError("out must be a contiguous tensor of q's shape and type")
         if scale is not None and not scale > 0.0:
             raise ValueError("scale must be positive")
-        with _Launch(device, stream) as sp:
-            need = lib.phyai_paged_attention_workspace_bytes(self._desc_ptr, Hq, T, B, most)
+        need = self._work.get((Hq, T, B, most))
+        with _launch(device, stream) as sp:
+            if need is None:
+                if len(self._work) >= 4096:
+                    self._work.clear()
+                need = self._work[Hq, T, B, most] = lib.phyai_paged_attention_workspace_bytes(self._desc_ptr, Hq, T, B, most)
             work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
             if out is None:
-                out = torch.empty(T, Hq, dh, dtype=q.dtype, device=device)
-            _paged_check(lib, lib.phyai_paged_attention(self._desc_ptr, layer, Hq, T, q.data_ptr(), row, B, cu, lens, table, most, 1 if causal else 0,
-                                                        prefix, 0.0 if scale is None else scale, out.data_ptr(), _ptr(work), need,
-                                                        self._status_ptr, sp))
+                out = torch.empty(shape, dtype=self.dtype, device=device)
+            st = lib.phyai_paged_attention(self._desc_ptr, layer, Hq, T, q.data_ptr(), row, B, cu, lens, table, most, 1 if causal else 0, prefix,
+                                           0.0 if scale is None else scale, out.data_ptr(), work.data_ptr() if need else None, need,
+                                           self._status_ptr, sp)
+        if st != OK:
+            _paged_fail(lib, st)
         return out
 
     def pack(self, page_table: torch.Tensor, kv_lens: torch.Tensor, kv_tokens: int, out: Optional[torch.Tensor] = None, stream=None):
@@ -684,11 +733,13 @@ class PagedCache:
         shape = (self.n_layers, 2, kv_tokens, self.n_kv_heads, self.head_dim)
         if out is not None and (out.shape != shape or out.dtype != self.dtype or out.device != device or not out.is_contiguous()):
             raise ValueError("out must be a contiguous tensor [L, 2, kv_tokens, Hkv, dh] of the cache's type")
-        with _Launch(device, stream) as sp:
+        with _launch(device, stream) as sp:
             if out is None:
                 out = torch.empty(shape, dtype=self.dtype, device=device)
             cu = torch.empty(B + 1, dtype=torch.int32, device=device)
-            _paged_check(lib, lib.phyai_pack_paged_kv(self._desc_ptr, B, lens, table, most, out.data_ptr(), kv_tokens, cu.data_ptr(), self._status_ptr, sp))
+            st = lib.phyai_pack_paged_kv(self._desc_ptr, B, lens, table, most, out.data_ptr(), kv_tokens, cu.data_ptr(), self._status_ptr, sp)
+        if st != OK:
+            _paged_fail(lib, st)
         return out, cu
 
 

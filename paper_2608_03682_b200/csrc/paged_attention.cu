@@ -11,11 +11,13 @@
 //                    fill the instruction; as Q K^T half of it would be empty
 //   P^T              transposed in registers (movmatrix) into the B operand of
 //   O^T += V^T P^T   V^T by transposing ldmatrix
-// The warps of a block merge through shared memory, the blocks of a row (key ranges) through a second kernel.
+// The warps of a block merge through shared memory, the blocks of a cluster through distributed shared memory, several clusters of a
+// row (key ranges) through a second kernel.
 #include <cstdio>
 
 #include "paged.cuh"
 #include "attention.cuh"
+#include "tc_pair.cuh"
 #include "tmap.h"
 
 namespace phyai {
@@ -39,28 +41,43 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, i
 constexpr int FW = 4;                    // warps of a block
 template <int DH>
 struct Few {
-  static constexpr int STAGES = DH == 256 ? 3 : DH == 128 ? 5 : 8;
-  static constexpr int TILE = 16 * DH * 2;                 // 16 keys (or values): blocks of 64 channels [DH / 64][16][128 B], swizzled
-  static constexpr int RING = STAGES * 2 * TILE;           // per warp
+  static constexpr int TILE = 16 * DH * 2;                 // 16 keys or values: blocks of 64 channels [DH / 64][16][128 B], swizzled
+  static constexpr int SLOTS = 24576 / TILE;               // of a warp's ring: K and V tiles in turn; 96 KB a block, two blocks an SM
+  static constexpr int RING = SLOTS * TILE;
   static constexpr size_t SMEM = 1024 + (size_t)FW * RING;
 };
-constexpr int FEW_LEAST = 2 * FW;        // tiles of 16 keys in a range, at least
+constexpr int FEW_LEAST = 2;             // tiles of 16 keys per warp in a range, at least
 
+__device__ __forceinline__ float ld_remote(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 ld_remote4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// A cluster of `csize` blocks takes the keys of one range of a row tile, each block a part of them.
 template <int DH, int NT>
-__global__ void __launch_bounds__(FW * 32) k_paged_few(const PagedAttn a, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(FW * 32, 2) k_paged_few(const PagedAttn a, const __grid_constant__ CUtensorMap map, const int csize) {
   using F = Few<DH>;
-  constexpr int RT = 8 * NT, KS = DH / 16, ST = F::STAGES;
+  constexpr int RT = 8 * NT, KS = DH / 16, NS = F::SLOTS, PITCH = DH + 4;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t full[FW][ST];
-  __shared__ float s_m[FW][RT], s_l[FW][RT];
+  __shared__ __align__(8) uint64_t full[FW][NS];
+  __shared__ float s_m[FW][RT], s_l[FW][RT], s_M[RT], s_L[RT];
   __shared__ int abort_flag, s_again[RT];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int hk = blockIdx.y;
-  const uint32_t ring = ((smem_u32(smem_raw) + 1023u) & ~1023u) + (uint32_t)warp * F::RING;
+  const int hk = blockIdx.y, unit = blockIdx.x / csize, rank = blockIdx.x - unit * csize;
+  const uint32_t ring0 = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = ring0 + (uint32_t)warp * F::RING;
   pdl_launch_dependents();
   if (threadIdx.x == 0) abort_flag = 0;
   if (lane == 0) {
-    for (int i = 0; i < ST; ++i) mbar_init(smem_u32(&full[warp][i]), 1);
+    for (int i = 0; i < NS; ++i) mbar_init(smem_u32(&full[warp][i]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (threadIdx.x < RT) s_again[threadIdx.x] = 0;
@@ -69,20 +86,20 @@ __global__ void __launch_bounds__(FW * 32) k_paged_few(const PagedAttn a, const 
   const WaitCtx wc{a.status, &abort_flag, a.wait_limit};
   PagedRequest r;
   int tile;
-  const bool skip = status_set(a.status);
-  if (!paged_unit<RT>(a, blockIdx.x, r, tile)) {
+  if (!paged_unit<RT>(a, unit, r, tile)) {
     if (threadIdx.x == 0) atomicExch(a.status, ST_INVALID_ARG);
     return;
   }
-  if (r.b < 0 || skip) return;
+  if (r.b < 0) return;
   const int rows = min(RT, r.n * a.group - tile * RT), row0 = tile * RT;
   const int n_keys = r.limit((row0 + rows - 1) / a.group, a.causal);              // (limits grow with the row)
-  const int tiles = (n_keys + 15) >> 4, ranges = ranges_of(tiles, a.ranges, FEW_LEAST), range = blockIdx.z;
-  if (range >= ranges) return;
-  const int t0 = (int)((long long)tiles * range / ranges), t1 = (int)((long long)tiles * (range + 1) / ranges);
+  const int tiles = (n_keys + 15) >> 4, ranges = ranges_of(tiles, a.ranges, FEW_LEAST * FW * csize), range = blockIdx.z;
+  if (range >= ranges) return;                                                    // (the whole cluster)
+  const int c0 = (int)((long long)tiles * range / ranges), c1 = (int)((long long)tiles * (range + 1) / ranges);       // tiles of the cluster, of this block
+  const int t0 = c0 + (int)((long long)(c1 - c0) * rank / csize), t1 = c0 + (int)((long long)(c1 - c0) * (rank + 1) / csize);
   const int mine = (t1 - t0 - warp + FW - 1) / FW;                                // tiles t0 + warp, + FW, ...
 
-  // ---- copies: one of K, one of V per tile.  Table entries come 32 tiles at a time, one per lane.
+  // ---- copies: K and V of a tile in turn.  Table entries come 32 tiles at a time, one per lane.
   const size_t trow = (size_t)r.b * a.pb.max_pages;
   int page_of = 0;
   auto fetch_pages = [&](int i0) {
@@ -93,19 +110,19 @@ __global__ void __launch_bounds__(FW * 32) k_paged_few(const PagedAttn a, const 
       page_of = a.pb.n_pages;                                                     // (past the planes: the copy fills in zeros)
     }
   };
-  auto issue = [&](int i) {
-    if ((i & 31) == 0) fetch_pages(i);
+  auto issue = [&](int j) {                                                       // copy j: K (even) or V (odd) of tile j / 2
+    const int i = j >> 1;
+    if ((i & 31) == 0 && !(j & 1)) fetch_pages(i);
     const int page = __shfl_sync(0xffffffffu, page_of, i & 31);
     if (lane == 0) {
-      const int key = (t0 + warp + i * FW) << 4, st = i % ST;
+      const int key = (t0 + warp + i * FW) << 4, sl = j % NS;
       const int row = (int)(((long long)page << a.pb.page_shift) + (key & ((1 << a.pb.page_shift) - 1)));
-      const uint32_t bar = smem_u32(&full[warp][st]), dst = ring + (uint32_t)st * (2 * F::TILE);
-      mbar_expect_tx(bar, 2 * F::TILE);
-      tma_rows(dst, &map, row, hk * (DH / 64), a.plane, bar);
-      tma_rows(dst + F::TILE, &map, row, hk * (DH / 64), a.plane + 1, bar);
+      const uint32_t bar = smem_u32(&full[warp][sl]);
+      mbar_expect_tx(bar, F::TILE);
+      tma_rows(ring + (uint32_t)sl * F::TILE, &map, row, hk * (DH / 64), a.plane + (j & 1), bar);
     }
   };
-  for (int i = 0; i < min(ST, mine); ++i) issue(i);
+  for (int j = 0; j < min(NS, 2 * mine); ++j) issue(j);
 
   // ---- Q^T as B operand: lane (g, t) holds channels 16 kk + 2 t, + 1 and + 8, + 9 of row g
   uint32_t qf[NT][KS][2];
@@ -136,17 +153,9 @@ __global__ void __launch_bounds__(FW * 32) k_paged_few(const PagedAttn a, const 
   const int rowk = lane & 15, chk = lane >> 4;                       // ldmatrix of K: keys 0-15, chunks 2 kk, 2 kk + 1
   const int rowv = (lane & 7) + ((lane >> 4) << 3), chv = (lane >> 3) & 1;   // of V: (keys 0-7, ch 0-7), (0-7, 8-15), (8-15, 0-7), (8-15, 8-15)
   for (int it = 0; it < mine; ++it) {
-    const int st = it % ST, key0 = (t0 + warp + it * FW) << 4;
-    const uint32_t ks = ring + (uint32_t)st * (2 * F::TILE), vs = ks + F::TILE;
-    mbar_wait_drain(smem_u32(&full[warp][st]), (uint32_t)(it / ST) & 1u, wc);
-    if (key0 + 16 > r.kv) {                                          // rows past the cached tokens hold anything: their values become zeros
-      const int keep = r.kv - key0;
-      for (int i = lane; i < (16 - keep) * (DH / 8); i += 32) {
-        const int row = keep + i / (DH / 8), ch = i % (DH / 8);
-        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(vs + (uint32_t)((ch >> 3) * 2048 + row * 128 + (ch & 7) * 16)), "r"(0u) : "memory");
-      }
-      __syncwarp();
-    }
+    const int jk = 2 * it, jv = jk + 1, key0 = (t0 + warp + it * FW) << 4;
+    const uint32_t ks = ring + (uint32_t)(jk % NS) * F::TILE, vs = ring + (uint32_t)(jv % NS) * F::TILE;
+    mbar_wait_drain(smem_u32(&full[warp][jk % NS]), (uint32_t)(jk / NS) & 1u, wc);
     float s[NT][2][4] = {};
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
@@ -156,6 +165,8 @@ __global__ void __launch_bounds__(FW * 32) k_paged_few(const PagedAttn a, const 
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) mma_bf16(s[nt][kk & 1], kf, qf[nt][kk][0], qf[nt][kk][1]);
     }
+    __syncwarp();
+    if (jk + NS < 2 * mine) issue(jk + NS);
     uint32_t pf[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -185,6 +196,15 @@ __global__ void __launch_bounds__(FW * 32) k_paged_few(const PagedAttn a, const 
       pf[nt][0] = transpose8x8(pack_bf16(x[0], x[1]));
       pf[nt][1] = transpose8x8(pack_bf16(x[2], x[3]));
     }
+    mbar_wait_drain(smem_u32(&full[warp][jv % NS]), (uint32_t)(jv / NS) & 1u, wc);
+    if (key0 + 16 > r.kv) {                                          // rows past the cached tokens hold anything: their values become zeros
+      const int keep = r.kv - key0;
+      for (int i = lane; i < (16 - keep) * (DH / 8); i += 32) {
+        const int row = keep + i / (DH / 8), ch = i % (DH / 8);
+        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(vs + (uint32_t)((ch >> 3) * 2048 + row * 128 + (ch & 7) * 16)), "r"(0u) : "memory");
+      }
+      __syncwarp();
+    }
 #pragma unroll
     for (int ct = 0; ct < KS; ++ct) {
       uint32_t vf[4];
@@ -194,14 +214,13 @@ __global__ void __launch_bounds__(FW * 32) k_paged_few(const PagedAttn a, const 
       for (int nt = 0; nt < NT; ++nt) mma_bf16(acc[nt][ct], vf, pf[nt][0], pf[nt][1]);
     }
     __syncwarp();
-    if (it + ST < mine) issue(it + ST);
+    if (jv + NS < 2 * mine) issue(jv + NS);
   }
 
   // ---- the warps' results: rows of DH fp32 (4 more: free of bank conflicts) in each warp's own ring
-  constexpr int PITCH = DH + 4;
   static_assert(RT * PITCH * 4 <= F::RING, "a warp's partial result exceeds its ring");
-  float* const part = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
-  float* const part0 = reinterpret_cast<float*>(smem_raw + (ring - (uint32_t)warp * F::RING - smem_u32(smem_raw)));
+  float* const part0 = reinterpret_cast<float*>(smem_raw + (ring0 - smem_u32(smem_raw)));
+  float* const part = part0 + (size_t)warp * (F::RING / 4);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -216,20 +235,53 @@ __global__ void __launch_bounds__(FW * 32) k_paged_few(const PagedAttn a, const 
       for (int e = 0; e < 4; ++e) part[(nt * 8 + 2 * t + (e & 1)) * PITCH + ct * 16 + g + (e >> 1) * 8] = acc[nt][ct][e];
   }
   __syncthreads();
-  if (*reinterpret_cast<volatile int*>(&abort_flag)) return;
+  // (block) the warps' partial results merged, in place of the first
   for (int i = threadIdx.x; i < rows * (DH / 4); i += FW * 32) {
     const int rr = i / (DH / 4), c = (i % (DH / 4)) * 4;
-    float M = -INFINITY, w[FW], sum = 0.f;
+    float M = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int k = 0; k < FW; ++k) M = fmaxf(M, s_m[k][rr]);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < FW; ++k) {
-      w[k] = s_m[k][rr] == -INFINITY ? 0.f : ex2_fast(s_m[k][rr] - M);
-      sum += w[k] * s_l[k][rr];
+      const float w = s_m[k][rr] == -INFINITY ? 0.f : ex2_fast(s_m[k][rr] - M);
+      sum += w * s_l[k][rr];
       const float4 v = *reinterpret_cast<const float4*>(part0 + (size_t)k * (F::RING / 4) + rr * PITCH + c);
-      o.x += w[k] * v.x, o.y += w[k] * v.y, o.z += w[k] * v.z, o.w += w[k] * v.w;
+      o.x += w * v.x, o.y += w * v.y, o.z += w * v.z, o.w += w * v.w;
     }
+    *reinterpret_cast<float4*>(part0 + rr * PITCH + c) = o;
+    if (c == 0) s_M[rr] = M, s_L[rr] = sum;
+  }
+  // (cluster) each block takes a part of the channels
+  if (csize > 1) cluster_sync_all();
+  else __syncthreads();
+  const bool skip = status_set(a.status) || *reinterpret_cast<volatile int*>(&abort_flag);   // (no partial result of a call that has failed)
+  for (int i = rank * (FW * 32) + threadIdx.x; i < rows * (DH / 4); i += csize * (FW * 32)) {
+    const int rr = i / (DH / 4), c = (i % (DH / 4)) * 4;
+    float M = s_M[rr], sum = s_L[rr];
+    float4 o;
+    if (csize == 1) {
+      o = *reinterpret_cast<const float4*>(part0 + rr * PITCH + c);
+    } else {
+      const uint32_t am = smem_u32(&s_M[rr]), al = smem_u32(&s_L[rr]), ao = ring0 + (uint32_t)(rr * PITCH + c) * 4u;
+      float ms[8], ls[8];
+      float4 os[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < csize) ms[k] = ld_remote(map_rank(am, k)), ls[k] = ld_remote(map_rank(al, k)), os[k] = ld_remote4(map_rank(ao, k));
+      M = -INFINITY, sum = 0.f, o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < csize) M = fmaxf(M, ms[k]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < csize) {
+          const float w = ms[k] == -INFINITY ? 0.f : ex2_fast(ms[k] - M);
+          sum += w * ls[k];
+          o.x += w * os[k].x, o.y += w * os[k].y, o.z += w * os[k].z, o.w += w * os[k].w;
+        }
+    }
+    if (skip) continue;
     // (0 x infinity and 0 x NaN of keys that this row does not see, or of its own: told apart below)
     if (a.causal && !(fabsf(o.x) + fabsf(o.y) + fabsf(o.z) + fabsf(o.w) < INFINITY)) s_again[rr] = 1;
     const int tok = r.lo + (row0 + rr) / a.group, h = hk * a.group + (row0 + rr) % a.group;
@@ -241,15 +293,17 @@ __global__ void __launch_bounds__(FW * 32) k_paged_few(const PagedAttn a, const 
     }
     if (c == 0 && a.ranges > 1) a.part_ml[((size_t)range * a.pb.tokens + tok) * a.hq + h] = make_float4(M, sum, (float)ranges, 0.f);
   }
+  // no block leaves while another reads its shared memory; and the rows below are written over all channels
+  if (csize > 1) cluster_sync_all();
+  else __syncthreads();
   if (!a.causal) return;
-  __syncthreads();
   for (int rr = warp; rr < rows; rr += FW) {
     if (!s_again[rr]) continue;
-    const int i = (row0 + rr) / a.group, hidden = max(t0 * 16, r.limit(i, 1));
-    if (!paged_hidden_odd<DH / 32, __nv_bfloat16>(a, r.b, hk, DH, 0, hidden, min(t1 * 16, r.kv))) continue;
+    const int i = (row0 + rr) / a.group, hidden = max(c0 * 16, r.limit(i, 1));
+    if (!paged_hidden_odd<DH / 32, __nv_bfloat16>(a, r.b, hk, DH, 0, hidden, min(c1 * 16, r.kv))) continue;
     const int tok = r.lo + i, h = hk * a.group + (row0 + rr) % a.group, c = lane * (DH / 32);
     float o[DH / 32], M, sum;
-    paged_row_alone<DH>(a, r.b, (const __nv_bfloat16*)a.q + tok * a.q_stride + (long long)h * DH, hk, t0 * 16, min(t1 * 16, r.limit(i, 1)), o, M, sum);
+    paged_row_alone<DH>(a, r.b, (const __nv_bfloat16*)a.q + tok * a.q_stride + (long long)h * DH, hk, c0 * 16, min(c1 * 16, r.limit(i, 1)), o, M, sum);
     const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
 #pragma unroll
     for (int e = 0; e < DH / 32; ++e) {
@@ -464,11 +518,12 @@ phyai_status_t bad_arg(const char* m) {
 
 // What a call launches: the kernel's row tile, its units and key ranges.
 struct Plan {
-  int f32, pair, rt, ranges;
+  int f32, pair, rt, ranges, csize;      // csize: blocks of a cluster, which share a range
   long long units;
 };
 Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int max_pages, int n_sm) {
   Plan p{};
+  p.csize = 1;
   const int group = hq / (int)c->n_kv_heads, holders = tokens < batch ? tokens : batch;      // requests with tokens, at most
   const long long rows = (long long)tokens * group;
   p.f32 = c->dtype == PHYAI_F32;
@@ -485,17 +540,21 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
     return p;
   }
   if (p.f32) {
-    p.rt = rows > 16ll * holders ? 64 : 16;
+    // tiles of 64 rows where there are enough of them for the SMs (17 tokens of 4 heads of 4 requests: 16-row tiles)
+    p.rt = rows / 64 * c->n_kv_heads >= n_sm ? 64 : 16;
   } else {
     const int most = c->head_dim == 64 ? 32 : 16;
     p.rt = rows <= 8ll * holders ? 8 : rows <= 16ll * holders || most == 16 ? 16 : most;
   }
   p.units = rows / p.rt + holders;
-  // key ranges: enough blocks for two rounds of the SMs, of at least 128 keys
+  // parts of a row tile's keys: enough blocks for two on each SM, of at least 128 keys; up to eight of them are a cluster
   const long long full = (rows + p.rt - 1) / p.rt > holders ? (rows + p.rt - 1) / p.rt : holders, blocks = full * c->n_kv_heads;
-  long long ranges = (2ll * n_sm + blocks - 1) / blocks;
-  if (ranges > keys / 128) ranges = keys / 128;
-  p.ranges = (int)(ranges < 1 ? 1 : ranges > 64 ? 64 : ranges);
+  long long parts = (2ll * n_sm + blocks - 1) / blocks;
+  if (parts > keys / 128) parts = keys / 128;
+  if (!p.f32)
+    while (p.csize < 8 && 2 * p.csize <= parts) p.csize *= 2;
+  parts /= p.csize;
+  p.ranges = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
   return p;
 }
 size_t partial_bytes(const Plan& p, int hq, int dh, int tokens) {
@@ -513,7 +572,14 @@ cudaError_t launch_few(const PagedAttn& a, const Plan& p, const CUtensorMap& map
     if (e != cudaSuccess) return e;
     once.done();
   }
-  return launch_pdl(k_paged_few<DH, NT>, dim3((unsigned)p.units, a.hkv, p.ranges), dim3(FW * 32), Few<DH>::SMEM, st, a, map);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)p.units * p.csize, a.hkv, p.ranges), cfg.blockDim = dim3(FW * 32), cfg.dynamicSmemBytes = Few<DH>::SMEM, cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization, at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = p.csize, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+  cfg.attrs = at, cfg.numAttrs = p.csize > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, k_paged_few<DH, NT>, a, map, p.csize);
 }
 template <int DH, int RR>
 cudaError_t launch_f32(const PagedAttn& a, const Plan& p, cudaStream_t st) {

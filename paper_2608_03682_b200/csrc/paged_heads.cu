@@ -5,9 +5,9 @@
 //
 // A head x of dh channels becomes  y = x * rsqrt(mean(x^2) + eps) * (1 + gain)  and then, for j < dh / 2,
 //   (y_j, y_{j + dh/2}) -> (y_j cos - y_{j + dh/2} sin, y_{j + dh/2} cos + y_j sin)  with the table's row of its position.
-// Everything is read once and written once, so memory bounds it: a group of dh / 8 lanes takes a head, 8 channels a lane (16-byte
-// accesses of bf16), the sum of squares and the rotary partner come by shuffles (the partner channels sit dh / 16 lanes away), and the
-// arithmetic is fp32 with one rounding at the store.
+// Everything is read once and written once, so memory bounds it: a lane takes 16 bytes of a head's
+// channels and their rotary partners, so that only the sum of squares crosses lanes (with 8 channels a lane and the
+// partners by shuffles, shuffles and table loads bounded it).  The arithmetic is fp32 with one rounding at the store.
 #include <cstdio>
 
 #include "../../include/phyai.h"
@@ -19,36 +19,42 @@ thread_local char g_paged_err[256] = "";
 
 namespace {
 
-// 8 consecutive channels
-struct F8 {
-  float v[8];
+// 16 bytes of consecutive channels, as stored
+template <typename T>
+struct Raw;
+template <>
+struct Raw<float> {
+  static constexpr int N = 4;
+  float4 a;
+  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w; }
 };
-__device__ __forceinline__ F8 load8(const float* p) {
-  F8 r;
-  *reinterpret_cast<float4*>(r.v) = *reinterpret_cast<const float4*>(p);
-  *reinterpret_cast<float4*>(r.v + 4) = *reinterpret_cast<const float4*>(p + 4);
-  return r;
-}
-__device__ __forceinline__ F8 load8(const __nv_bfloat16* p) {
-  const uint4 w = *reinterpret_cast<const uint4*>(p);
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-  F8 r;
+template <>
+struct Raw<__nv_bfloat16> {
+  static constexpr int N = 8;
+  uint4 a;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) r.v[2 * i] = __uint_as_float(u[i] << 16), r.v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-  return r;
-}
-__device__ __forceinline__ void store8(float* p, const F8& x) {
-  *reinterpret_cast<float4*>(p) = *reinterpret_cast<const float4*>(x.v);
-  *reinterpret_cast<float4*>(p + 4) = *reinterpret_cast<const float4*>(x.v + 4);
-}
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const F8& x) {
-  uint32_t u[4];
+    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(u[i] << 16), v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+  }
+};
+template <int N>
+__device__ __forceinline__ void store_channels(float* p, const float (&x)[N]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 b = __floats2bfloat162_rn(x.v[2 * i], x.v[2 * i + 1]);
+  for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+}
+template <int N>
+__device__ __forceinline__ void store_channels(__nv_bfloat16* p, const float (&x)[N]) {
+  uint32_t u[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
     u[i] = *reinterpret_cast<const uint32_t*>(&b);
   }
-  *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+  if constexpr (N == 8) *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+  else *reinterpret_cast<uint2*>(p) = make_uint2(u[0], u[1]);
 }
 
 struct HeadsArgs {
@@ -66,19 +72,18 @@ struct HeadsArgs {
   int* status;
 };
 
-constexpr int HT = 256;                  // threads of a block
+constexpr int HT = 256, HB = 3;          // threads of a block, blocks of an SM
 
-// A warp takes a token's heads, 32 / (dh / 8) at a time (a "slot" is such a set); a unit is U slots of one token, whose loads are all
-// issued before the first is used.
+// A lane takes 16 bytes of channels (C of them) and their rotary partners of a head, a warp 64 C / dh heads of a token at a time (a slot);
+// slots run over the tokens, a warp takes U in a row and issues all their loads before it uses the first.
 template <int DH, typename IN, typename OUT, bool APPEND, int U>
-__global__ void __launch_bounds__(HT) k_heads(const HeadsArgs a) {
-  constexpr int LANES = DH / 8, HPS = 32 / LANES;           // lanes per head, heads per slot
+__global__ void __launch_bounds__(HT, HB) k_heads(const HeadsArgs a) {
+  constexpr int C = Raw<IN>::N, HALF = DH / 2, LANES = HALF / C, HPS = 32 / LANES;           // lanes per head, heads per slot
   __shared__ int s_cu[APPEND ? PAGED_MAX_BATCH + 1 : 1], s_kv[APPEND ? PAGED_MAX_BATCH : 1];
   __shared__ int s_skip;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LANES, c = (lane % LANES) * 8;
-  const int H = (a.q ? a.hq : 0) + a.hkv + (a.v ? a.hkv : 0), hq = a.q ? a.hq : 0;
-  const int slots = (H + HPS - 1) / HPS, units_t = (slots + U - 1) / U;      // per token
-  const long long units = (long long)a.tokens * units_t;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LANES, c = (lane % LANES) * C;
+  const int hq = a.q ? a.hq : 0, H = hq + a.hkv + (a.v ? a.hkv : 0), slots = (H + HPS - 1) / HPS;
+  const int step = (int)gridDim.x * (HT / 32) * U, step_tok = step / slots, step_slot = step - step_tok * slots;
   pdl_launch_dependents();
   pdl_wait();
   if (threadIdx.x == 0) s_skip = status_set(a.status);
@@ -99,88 +104,100 @@ __global__ void __launch_bounds__(HT) k_heads(const HeadsArgs a) {
     __syncthreads();
   }
   if (s_skip) return;
-  const IN* const src[3] = {(const IN*)a.q, (const IN*)a.k, (const IN*)a.v};
 
-  for (long long unit = (long long)blockIdx.x * (HT / 32) + warp; unit < units; unit += (long long)gridDim.x * (HT / 32)) {
-    const int tok = (int)(unit / units_t), slot0 = (int)(unit - (long long)tok * units_t) * U;
-    F8 x[U];
-    int head[U], kind[U];
+  const int s0 = ((int)blockIdx.x * (HT / 32) + warp) * U;
+  for (int tok0 = s0 / slots, slot0 = s0 % slots; tok0 < a.tokens;) {
+    Raw<IN> lo[U], hi[U];
+    {
+      int tok = tok0, slot = slot0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = (slot0 + u) * HPS + sub;
-      kind[u] = h < hq ? 0 : h < hq + a.hkv ? 1 : h < H ? 2 : 3;
-      head[u] = kind[u] == 0 ? h : kind[u] == 1 ? h - hq : h - hq - a.hkv;
-      if (kind[u] < 3) {
-        const long long stride = kind[u] == 0 ? a.q_stride : kind[u] == 1 ? a.k_stride : a.v_stride;
-        x[u] = load8((kind[u] == 0 ? src[0] : kind[u] == 1 ? src[1] : src[2]) + tok * stride + head[u] * DH + c);
-      } else {
-        x[u] = F8{};
+      for (int u = 0; u < U; ++u) {
+        const int h = slot * HPS + sub;
+        if (h < H && tok < a.tokens) {
+          const IN* p = h < hq ? (const IN*)a.q + tok * a.q_stride + h * DH
+                               : h < hq + a.hkv ? (const IN*)a.k + tok * a.k_stride + (h - hq) * DH : (const IN*)a.v + tok * a.v_stride + (h - hq - a.hkv) * DH;
+          lo[u].load(p + c), hi[u].load(p + c + HALF);
+        } else {
+          lo[u] = hi[u] = Raw<IN>{};
+        }
+        if (++slot == slots) slot = 0, ++tok;
       }
     }
-    // ---- where the token is
-    int pos = 0;
+    float cs[C], sn[C];
     long long row = -1;
-    bool ok = true;
-    if constexpr (APPEND) {
-      int before = 0;                                        // requests that end at or before this token
-      for (int i0 = 0; i0 < a.pb.batch; i0 += 32) before += __popc(__ballot_sync(0xffffffffu, i0 + lane < a.pb.batch && s_cu[i0 + lane + 1] <= tok));
-      const int b = before;
-      if (tok < s_cu[0] || b >= a.pb.batch) continue;        // (a row of no request)
-      const int place = s_kv[b] - (s_cu[b + 1] - tok);
-      row = paged_row(a.pb, b, place);
-      pos = a.positions ? a.positions[tok] : place;
-      ok = row >= 0;
-    } else {
-      if (a.positions) pos = a.positions[tok];
-    }
-    if (a.rope && (unsigned)pos >= (unsigned)a.n_positions) ok = false;
-    if (!ok) {                                               // (the whole warp: nothing of this token is written)
-      if (lane == 0) atomicExch(a.status, ST_INVALID_ARG);
-      continue;
-    }
-    float cs[8], sn[8];
-    if (a.rope) {
-      const float4* t = reinterpret_cast<const float4*>(a.rope + ((size_t)pos * (DH / 2) + (c & (DH / 2 - 1))) * 2);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 w = __ldg(t + i);
-        cs[2 * i] = w.x, sn[2 * i] = w.y, cs[2 * i + 1] = w.z, sn[2 * i + 1] = w.w;
-      }
-      if (c < DH / 2) {                                      // y_j cos - y_{j + dh/2} sin in the lower half
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sn[i] = -sn[i];
-      }
-    }
+    bool ok = false;
+    int tok = tok0, slot = slot0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const float* gain = kind[u] == 0 ? a.q_gain : kind[u] == 1 ? a.k_gain : nullptr;
+      if (tok >= a.tokens) break;
+      if (u == 0 || slot == 0) {                                 // ---- another token: where it is
+        int pos = 0;
+        ok = true;
+        if constexpr (APPEND) {
+          int b = 0;                                             // requests that end at or before it
+          for (int i0 = 0; i0 < a.pb.batch; i0 += 32) b += __popc(__ballot_sync(0xffffffffu, i0 + lane < a.pb.batch && s_cu[min(i0 + lane, a.pb.batch - 1) + 1] <= tok));
+          ok = tok >= s_cu[0] && b < a.pb.batch;                 // (else a row of no request)
+          if (ok) {
+            const int place = s_kv[b] - (s_cu[b + 1] - tok);
+            row = paged_row(a.pb, b, place);
+            pos = a.positions ? a.positions[tok] : place;
+            if (row < 0 || (a.rope && (unsigned)pos >= (unsigned)a.n_positions)) {
+              if (lane == 0) atomicExch(a.status, ST_INVALID_ARG);
+              ok = false;                                        // (nothing of this token is written)
+            }
+          }
+        } else if (a.rope) {
+          pos = a.positions[tok];
+          if ((unsigned)pos >= (unsigned)a.n_positions) {
+            if (lane == 0) atomicExch(a.status, ST_INVALID_ARG);
+            ok = false;
+          }
+        }
+        if (ok && a.rope) {
+          const float4* t = reinterpret_cast<const float4*>(a.rope + ((size_t)pos * HALF + c) * 2);
+#pragma unroll
+          for (int i = 0; i < C / 2; ++i) {
+            const float4 w = __ldg(t + i);
+            cs[2 * i] = w.x, sn[2 * i] = w.y, cs[2 * i + 1] = w.z, sn[2 * i + 1] = w.w;
+          }
+        }
+      }
+      const int h = slot * HPS + sub, kind = h < hq ? 0 : h < hq + a.hkv ? 1 : h < H ? 2 : 3;
+      float x[C], y[C];
+      lo[u].get(x), hi[u].get(y);
+      const float* gain = kind == 0 ? a.q_gain : kind == 1 ? a.k_gain : nullptr;
       float ss = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(x[u].v[i], x[u].v[i], ss);
+      for (int i = 0; i < C; ++i) ss = fmaf(x[i], x[i], ss), ss = fmaf(y[i], y[i], ss);
 #pragma unroll
       for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
       if (gain) {
         const float r = rsqrtf(ss * (1.0f / DH) + a.eps);
-        const F8 g = load8(gain + c);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[u].v[i] *= r * (1.0f + g.v[i]);
-      }
-      if (a.rope) {
-        F8 y;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y.v[i] = __shfl_xor_sync(0xffffffffu, x[u].v[i], LANES / 2);
-        if (kind[u] < 2) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[u].v[i] = fmaf(y.v[i], sn[i], x[u].v[i] * cs[i]);
+        for (int i = 0; i < C; i += 4) {
+          const float4 g = __ldg(reinterpret_cast<const float4*>(gain + c + i)), f = __ldg(reinterpret_cast<const float4*>(gain + c + HALF + i));
+          x[i] *= fmaf(r, g.x, r), x[i + 1] *= fmaf(r, g.y, r), x[i + 2] *= fmaf(r, g.z, r), x[i + 3] *= fmaf(r, g.w, r);
+          y[i] *= fmaf(r, f.x, r), y[i + 1] *= fmaf(r, f.y, r), y[i + 2] *= fmaf(r, f.z, r), y[i + 3] *= fmaf(r, f.w, r);
         }
       }
-      if (kind[u] == 0) {
-        store8((OUT*)a.q_out + ((size_t)tok * a.hq + head[u]) * DH + c, x[u]);
-      } else if (kind[u] < 3) {
-        OUT* base = APPEND ? (OUT*)(kind[u] == 1 ? a.k_plane : a.v_plane) : (OUT*)a.k_out;
-        store8(base + ((size_t)(APPEND ? row : tok) * a.hkv + head[u]) * DH + c, x[u]);
+      if (a.rope && kind < 2) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+          const float t = x[i];
+          x[i] = fmaf(-y[i], sn[i], t * cs[i]);
+          y[i] = fmaf(t, sn[i], y[i] * cs[i]);
+        }
       }
+      if (ok && kind < 3) {
+        OUT* p = kind == 0 ? (OUT*)a.q_out + ((size_t)tok * a.hq + h) * DH
+                 : APPEND  ? (OUT*)(kind == 1 ? a.k_plane : a.v_plane) + ((size_t)row * a.hkv + (kind == 1 ? h - hq : h - hq - a.hkv)) * DH
+                           : (OUT*)a.k_out + ((size_t)tok * a.hkv + h - hq) * DH;
+        store_channels(p + c, x), store_channels(p + c + HALF, y);
+      }
+      if (++slot == slots) slot = 0, ++tok;
     }
+    tok0 += step_tok, slot0 += step_slot;
+    if (slot0 >= slots) slot0 -= slots, ++tok0;
   }
 }
 
@@ -199,15 +216,15 @@ namespace {
 
 template <int DH, typename IN, typename OUT, bool APPEND>
 cudaError_t launch_heads(const HeadsArgs& a, cudaStream_t st) {
-  constexpr int HPS = 32 / (DH / 8), U = 4;
+  constexpr int HPS = 64 * Raw<IN>::N / DH, U = 2;
   const int H = (a.q ? a.hq : 0) + a.hkv + (a.v ? a.hkv : 0), slots = (H + HPS - 1) / HPS, n_sm = paged_sm_count();
   if (n_sm <= 0) return cudaErrorInvalidDevice;
-  const long long per_warp = (long long)a.tokens * slots;
-  // Few tokens: a warp per slot, all of them at a time; many: four slots a warp.
-  if (per_warp <= (long long)n_sm * 16)
-    return launch_pdl(k_heads<DH, IN, OUT, APPEND, 1>, dim3((unsigned)((per_warp + HT / 32 - 1) / (HT / 32))), dim3(HT), 0, st, a);
-  const long long units = (long long)a.tokens * ((slots + U - 1) / U), blocks = (units + HT / 32 - 1) / (HT / 32);
-  const long long most = (long long)n_sm * 8;
+  const long long n = (long long)a.tokens * slots;
+  if (n > 0x7f000000ll) return cudaErrorInvalidValue;
+  // Few tokens: a warp per slot, all of them at a time; many: U slots a warp.
+  if (n <= (long long)n_sm * 16)
+    return launch_pdl(k_heads<DH, IN, OUT, APPEND, 1>, dim3((unsigned)((n + HT / 32 - 1) / (HT / 32))), dim3(HT), 0, st, a);
+  const long long blocks = (n + U * (HT / 32) - 1) / (U * (HT / 32)), most = (long long)n_sm * HB;
   return launch_pdl(k_heads<DH, IN, OUT, APPEND, U>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(HT), 0, st, a);
 }
 template <bool APPEND>
