@@ -16,7 +16,7 @@
 // rows whose result is not finite are looked at again after the last unit (see paged_row_alone).
 //
 // Few units (short chunks over long histories): a unit's keys are split over several pairs, the fp32 results are merged by k_paged_merge.
-// Warps of a CTA: 0 fetches K, 1 V, 2 Q, 3 issues the MMAs (leader CTA), 4-11 softmax, correction, output.  Every wait is bounded; after
+// Warps of a CTA: 0 fetches K and Q, 1 V; 3 issues the MMAs (leader CTA); 4-11 softmax, correction, output.  Every wait is bounded; after
 // a give-up the protocol runs to its end and only the global stores are skipped.
 #include <cstdio>
 
@@ -46,6 +46,33 @@ __device__ __forceinline__ void copy4d(uint32_t dst, const CUtensorMap* map, int
   asm volatile(
       "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+      : "memory");
+}
+
+// Four MMAs of K = 16 in a row (64 channels, or 64 keys), by the lane with `elected` (one election per product, no branch between
+// them: what a warp issues between two MMAs is what bounds it here).  `first`: the first one overwrites the accumulator.
+__device__ __forceinline__ void umma2_ss_x4(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t first, uint32_t elected) {
+  asm volatile(
+      "{\n.reg .pred e, p, q;\n.reg .b64 a1, a2, a3, b1, b2, b3;\n"
+      "setp.ne.b32 e, %5, 0;\nsetp.eq.b32 p, %4, 0;\nsetp.eq.b32 q, 0, 0;\n"
+      "add.s64 a1, %1, 2;\nadd.s64 b1, %2, 2;\nadd.s64 a2, %1, 4;\nadd.s64 b2, %2, 4;\nadd.s64 a3, %1, 6;\nadd.s64 b3, %2, 6;\n"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], a1, b1, %3, q;\n"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], a2, b2, %3, q;\n"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], a3, b3, %3, q;\n}" ::"r"(d),
+      "l"(da), "l"(db), "r"(idesc), "r"(first), "r"(elected)
+      : "memory");
+}
+__device__ __forceinline__ void umma2_ts_x4(uint32_t d, uint32_t ta, uint64_t db, uint32_t idesc, uint32_t first, uint32_t elected) {
+  asm volatile(
+      "{\n.reg .pred e, p, q;\n.reg .b32 a1, a2, a3;\n.reg .b64 b1, b2, b3;\n"
+      "setp.ne.b32 e, %5, 0;\nsetp.eq.b32 p, %4, 0;\nsetp.eq.b32 q, 0, 0;\n"
+      "add.s32 a1, %1, 8;\nadd.s64 b1, %2, 128;\nadd.s32 a2, %1, 16;\nadd.s64 b2, %2, 256;\nadd.s32 a3, %1, 24;\nadd.s64 b3, %2, 384;\n"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], [a1], b1, %3, q;\n"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], [a2], b2, %3, q;\n"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], [a3], b3, %3, q;\n}" ::"r"(d),
+      "r"(ta), "l"(db), "r"(idesc), "r"(first), "r"(elected)
       : "memory");
 }
 
@@ -187,7 +214,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   if (warp == 0) {
     // =========================== K: a buffer is free again once the logits of the tile two before exist ==================
     const int nc = np * (DH / 64 / cb), pc = lane % np, ch = (lane / np) * cb;        // copies of a block: one per lane
-    int k = 0, n = 0;
+    int k = 0, n = 0, i = 0;
     Unit u = next_unit(k);
     while (u.r.b >= 0) {
       for (int t = 0; t < u.T; ++t, ++n) {
@@ -198,6 +225,16 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
         if (half == 0 && lane == 0) mbar_expect_tx(bar, (uint32_t)L::TILE * 2);
         __syncwarp();
         if (lane < nc) copy4d(dst + (uint32_t)ch * L::KBLOCK + (uint32_t)pc * piece_bytes, &tmkv, row, u.hk * (DH / 64) + ch, a.plane, bar & LEADER_MASK);
+        if (t == 0) {                             // Q: its tile is free again once the last logits of the unit before exist
+          if (lane == 0) {
+            if (i > 0) mbar_wait_drain(smem_u32(&q_free), (uint32_t)(i - 1) & 1u, wl);
+            if (half == 0) mbar_expect_tx(smem_u32(&q_full), 2 * (uint32_t)(TOK * G * DH * 2));
+          }
+          __syncwarp();
+          if (lane < DH / 64)
+            copy4d(Qs + (uint32_t)lane * (128 * 128), &tmq, u.hk * G, u.r.lo + u.tok0 + half * TOK, lane, smem_u32(&q_full) & LEADER_MASK);
+          ++i;
+        }
       }
       u = next_unit(k);
     }
@@ -244,92 +281,59 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
       u = next_unit(k);
     }
     __syncwarp();
-  } else if (warp == 2) {
-    // =========================== Q: its tile is free again once the last logits of the unit before exist ==================
-    if (lane == 0) {
-      int k = 0, i = 0;
-      for (Unit u = next_unit(k); u.r.b >= 0; u = next_unit(k), ++i) {
-        if (i > 0) mbar_wait_drain(smem_u32(&q_free), (uint32_t)(i - 1) & 1u, wl);
-        const uint32_t bar = smem_u32(&q_full);
-        if (half == 0) mbar_expect_tx(bar, 2 * (uint32_t)(TOK * G * DH * 2));
-#pragma unroll
-        for (int c = 0; c < DH / 64; ++c) copy4d(Qs + (uint32_t)c * (128 * 128), &tmq, u.hk * G, u.r.lo + u.tok0 + half * TOK, c, bar & LEADER_MASK);
-      }
-    }
-    __syncwarp();
   } else if (warp == 3) {
     // =========================== MMA issuer (leader CTA): S(0), S(1), then P(n) V(n), S(n + 2), across the units ==========
+    // The products wait for one another through what stands between their MMAs: S(n + 2) follows P(n) V(n), whose P is in its buffer, in the
+    // pipe's order.  So the loop is short: plain waits in a fixed order, one election, four MMAs a statement.  (Whichever of the two had its
+    // operands first, an election per MMA: 600 to 900 clocks from the last MMA of a product to the first of the next, beside two busy warps of
+    // the scheduler, 3400 per tile.  Two warps, one per product: 2770, as S(n + 2) then waits for the completion of P(n) V(n).)
     if (half == 0) {
-      // S(n) may be issued once P V of tile n - 2 has been (its S buffer holds P of that tile).  Of the next logits and the next
-      // P V whichever has its operands goes first; logits when both have.
-      int k_s = 0, k_p = 0, ns = 0, is = 0, ts = 0, np_ = 0, ip = 0, tp = 0;      // tile of the call, unit, tile of the unit: of logits, of P V
-      Unit us = next_unit(k_s), up = us;
-      k_p = k_s;
-      uint32_t spins = 0;
-      while (up.r.b >= 0) {
-        if (us.r.b >= 0 && ns < np_ + 2) {
-          bool go = mbar_test(smem_u32(&k_full[ns & 1]), (uint32_t)(ns >> 1) & 1u) && (ts > 0 || mbar_test(smem_u32(&q_full), (uint32_t)is & 1u));
-          if (spins >= a.wait_limit) {             // given up: the protocol goes on in a fixed order
-            mbar_wait_drain(smem_u32(&k_full[ns & 1]), (uint32_t)(ns >> 1) & 1u, wc);
-            if (ts == 0) mbar_wait_drain(smem_u32(&q_full), (uint32_t)is & 1u, wc);
-            go = true;
-          }
-          if (__all_sync(0xffffffffu, go)) {
+      const uint32_t elected = elect_one() ? 1u : 0u;
+      int k = 0, ns = 0, is = 0, ts = 0;                          // logits: tile of the call, unit, tile of the unit
+      Unit us = next_unit(k);
+      auto logits = [&] {
+        mbar_wait_drain(smem_u32(&k_full[ns & 1]), (uint32_t)(ns >> 1) & 1u, wc);
+        if (ts == 0) mbar_wait_drain(smem_u32(&q_full), (uint32_t)is & 1u, wc);
+        tc_fence_after();
+        const uint64_t da = make_desc(Qs), db = make_desc(Ks + (uint32_t)(ns & 1) * L::TILE);      // (a 64-channel block further: 128 x 128 and 64 x 128 bytes)
+#pragma unroll
+        for (int c = 0; c < DH / 64; ++c)
+          umma2_ss_x4(tmem_s + (uint32_t)(ns & 1) * KB, da + (uint64_t)(c * ((128 * 128) >> 4)), db + (uint64_t)(c * (L::KBLOCK >> 4)), IDESC_S, c == 0 ? 1u : 0u, elected);
+        if (elected) umma2_commit(smem_u32(&s_full[ns & 1]));
+        ++ns;
+        if (++ts == us.T) {
+          if (elected) umma2_commit(smem_u32(&q_free));
+          ts = 0, ++is, us = next_unit(k);
+        }
+        __syncwarp();
+      };
+      int kp = 0;
+      Unit u = next_unit(kp);
+      if (us.r.b >= 0) logits();
+      for (int n = 0, i = 0; u.r.b >= 0; ++i) {
+        for (int t = 0; t < u.T; ++t, ++n) {
+          if (us.r.b >= 0) logits();                              // S(n + 1)
+          const uint32_t pf = smem_u32(&p_full[n & 1][0]), par = (uint32_t)(n >> 1) & 1u, vb = Vs + (uint32_t)(n & 1) * L::TILE;
+          mbar_wait_drain(smem_u32(&v_full[n & 1]), par, wc);
+          // (the tile in which the cached tokens end: rows of it were cleared by a warp of each CTA)
+          if (u.r.kv < (u.t0 + t + 1) * KB) pair_acquire(smem_u32(&v_full[n & 1]), par);
+          if (t == 0 && i > 0) mbar_wait_drain(smem_u32(&o_free), (uint32_t)(i - 1) & 1u, wc);
+#pragma unroll
+          for (int kh = 0; kh < 2; ++kh) {
+            mbar_wait_drain(pf + 8u * kh, par, wc);
             tc_fence_after();
-            const uint32_t kb = Ks + (uint32_t)(ns & 1) * L::TILE;
-            uint64_t da = make_desc(Qs), db = make_desc(kb);      // (a 64-channel block further: 128 x 128 and 64 x 128 bytes)
-#pragma unroll 1
-            for (int c = 0; c < DH / 64; ++c, da += (128 * 128) >> 4, db += L::KBLOCK >> 4) {
-#pragma unroll
-              for (int kk = 0; kk < 4; ++kk)
-                if (elect_one()) umma2_bf16(tmem_s + (uint32_t)(ns & 1) * KB, da + 2 * kk, db + 2 * kk, IDESC_S, (c > 0 || kk > 0) ? 1u : 0u);
-            }
-            if (elect_one()) umma2_commit(smem_u32(&s_full[ns & 1]));
-            if (ts + 1 == us.T && elect_one()) umma2_commit(smem_u32(&q_free));
-            __syncwarp();
-            ++ns;
-            if (++ts == us.T) ts = 0, ++is, us = next_unit(k_s);
-            if (spins < a.wait_limit) spins = 0;
-            continue;
+            // A = P of this tile: bf16 pairs in the first 64 columns of its S buffer
+            umma2_ts_x4(tmem_o, tmem_s + (uint32_t)(n & 1) * KB + (uint32_t)kh * 32, make_desc_mn(vb + (uint32_t)kh * L::PIECE, L::KBLOCK, 1024), IDESC_PV,
+                        t == 0 && kh == 0 ? 1u : 0u, elected);
           }
+          if (elected) umma2_commit(smem_u32(&pv_done[n & 1]));
+          __syncwarp();
         }
-        if (np_ < ns) {
-          const uint32_t pf = smem_u32(&p_full[np_ & 1][0]), par = (uint32_t)(np_ >> 1) & 1u;
-          bool go = mbar_test(smem_u32(&v_full[np_ & 1]), par) && mbar_test(pf, par) && (tp > 0 || ip == 0 || mbar_test(smem_u32(&o_free), (uint32_t)(ip - 1) & 1u));
-          if (spins >= a.wait_limit) {
-            mbar_wait_drain(smem_u32(&v_full[np_ & 1]), par, wc);
-            mbar_wait_drain(pf, par, wc);
-            if (tp == 0 && ip > 0) mbar_wait_drain(smem_u32(&o_free), (uint32_t)(ip - 1) & 1u, wc);
-            go = true;
-          }
-          if (__all_sync(0xffffffffu, go)) {
-            // (the tile in which the cached tokens end: rows of it were cleared by a warp of each CTA)
-            if (up.r.kv < (up.t0 + tp + 1) * KB) pair_acquire(smem_u32(&v_full[np_ & 1]), par);
-            const uint32_t vb = Vs + (uint32_t)(np_ & 1) * L::TILE;
-#pragma unroll 1
-            for (int kh = 0; kh < 2; ++kh) {
-              if (kh == 1) mbar_wait_drain(pf + 8u, par, wc);
-              tc_fence_after();
-              // A = P of this tile: bf16 pairs in the first 64 columns of its S buffer
-              const uint64_t db = make_desc_mn(vb + (uint32_t)kh * L::PIECE, L::KBLOCK, 1024);
-              const uint32_t tp_ = tmem_s + (uint32_t)(np_ & 1) * KB + (uint32_t)kh * 32;
-#pragma unroll
-              for (int kj = 0; kj < KB / 32; ++kj)
-                if (elect_one()) umma2_ts(tmem_o, tp_ + (uint32_t)kj * 8, db + kj * ((16 * 128) >> 4), IDESC_PV, (tp > 0 || kh > 0 || kj > 0) ? 1u : 0u);
-            }
-            if (elect_one()) umma2_commit(smem_u32(&pv_done[np_ & 1]));
-            __syncwarp();
-            ++np_;
-            if (++tp == up.T) tp = 0, ++ip, up = next_unit(k_p);
-            if (spins < a.wait_limit) spins = 0;
-            continue;
-          }
-        }
-        ++spins;
+        u = next_unit(kp);
       }
     }
     __syncwarp();
-  } else {
+  } else if (warp >= 4) {
     // =========================== softmax / correction / output ==============================================================
     const int g = (warp - 4) >> 2;            // which half of a row's columns: block g of a tile
     const int q = warp & 3;
@@ -340,6 +344,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     const uint32_t ostage = Qs + L::QTILE + (uint32_t)(warp - 4) * L::STG;
     const int c0 = g * (DH / 2);              // first of this warp's output channels
     float m = -INFINITY, l = 0.f, m_prev = 0.f, l_prev = 0.f;             // running maximum (log2 units) and sum (of this thread's columns)
+    int out_off[4];                           // where this lane stores of a unit's rows (lane / 4 + 8 x of the warp's 32)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int r = q * 32 + (lane >> 2) + 8 * x, rt = r / G;
+      out_off[x] = (rt * a.hq + r - rt * G) * DH + (lane & 3) * 8;
+    }
     bool odd = false;
     int k = 0, n = 0, i = 0;
     Unit u = next_unit(k), prev = u;
@@ -370,51 +380,63 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
         tc_fence_after();
         const bool okf = !skip && !*reinterpret_cast<volatile int*>(&abort_flag);
         const int first_tok = prev.r.lo + prev.tok0 + half * TOK, n_rows = okf ? min(TOK, prev.r.n - prev.tok0 - half * TOK) * G : 0;
-        const bool whole = prev.ranges == 1;
-        const size_t slot = ((size_t)prev.range * a.pb.tokens + first_tok + row_tok) * a.hq + prev.hk * G + (row - row_tok * G);
-        if (g == 0 && a.ranges > 1 && row < n_rows) a.part_ml[slot] = make_float4(m_prev, sum, (float)prev.ranges, 0.f);
-        const uint32_t rowp = ostage + (uint32_t)lane * 64u;
+        float fin = 0.f;
+        if (prev.ranges > 1) {
+          const size_t slot = ((size_t)prev.range * a.pb.tokens + first_tok + row_tok) * a.hq + prev.hk * G + (row - row_tok * G);
+          if (g == 0 && row < n_rows) a.part_ml[slot] = make_float4(m_prev, sum, (float)prev.ranges, 0.f);
 #pragma unroll 1
-        for (int c = 0; c < DH / 2; c += 32) {
-          float o[32];
-          tmem_ld32(tmem_o + lane_addr + (uint32_t)(c0 + c), o);
-          if (c + 32 == DH / 2) {                   // the accumulator may be overwritten
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) remote_arrive(ofree0);
-          }
-          float fin = 0.f;
-#pragma unroll
-          for (int e = 0; e < 32; ++e) fin += fabsf(o[e]);
-          odd |= row < n_rows && !(fin < INFINITY);
-          if (!whole) {
+          for (int c = 0; c < DH / 2; c += 32) {
+            float o[32];
+            tmem_ld32(tmem_o + lane_addr + (uint32_t)(c0 + c), o);
             if (row < n_rows) {
               float* p = a.part_o + slot * DH + c0 + c;
 #pragma unroll
               for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
             }
-            continue;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) fin += fabsf(o[e]);
           }
-#pragma unroll
-          for (int e = 0; e < 32; e += 8)
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(rowp + (uint32_t)(((e >> 3) ^ ((lane >> 1) & 3)) << 4)),
-                         "r"(pack_bf16(o[e] * inv, o[e + 1] * inv)), "r"(pack_bf16(o[e + 2] * inv, o[e + 3] * inv)),
-                         "r"(pack_bf16(o[e + 4] * inv, o[e + 5] * inv)), "r"(pack_bf16(o[e + 6] * inv, o[e + 7] * inv))
-                         : "memory");
+          tc_fence_before();
           __syncwarp();
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int rr = (lane >> 2) + 8 * x, ch = lane & 3, r = q * 32 + rr;
-            uint4 v;
-            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                         : "r"(ostage + (uint32_t)(rr * 64 + ((ch ^ ((rr >> 1) & 3)) << 4))) : "memory");
-            if (r < n_rows) {
-              const int rt = r / G;
-              *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + ((size_t)(first_tok + rt) * a.hq + prev.hk * G + (r - rt * G)) * DH + c0 + c + ch * 8) = v;
+          if (lane == 0) remote_arrive(ofree0);     // the accumulator may be overwritten
+        } else {
+          if (g == 0 && a.ranges > 1 && row < n_rows)
+            a.part_ml[((size_t)first_tok + row_tok) * a.hq + prev.hk * G + (row - row_tok * G)] = make_float4(m_prev, sum, 1.f, 0.f);
+          __nv_bfloat16* ob = (__nv_bfloat16*)a.out + ((size_t)first_tok * a.hq + prev.hk * G) * DH + c0;
+          const uint32_t rowp = ostage + (uint32_t)lane * 64u;
+          // (a rolled loop: run once per unit, its code comes from far at about 11 clocks an instruction; unrolled it took 5000 clocks)
+#pragma unroll 1
+          for (int c = 0; c < DH / 2; c += 32, ob += 32) {
+            float o[32], f4[4] = {0.f, 0.f, 0.f, 0.f};
+            tmem_ld32(tmem_o + lane_addr + (uint32_t)(c0 + c), o);
+            if (c + 32 == DH / 2) {                   // the accumulator may be overwritten
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) remote_arrive(ofree0);
             }
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) f4[j & 3] += fabsf(o[e + j]);
+              asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(rowp + (uint32_t)(((e >> 3) ^ ((lane >> 1) & 3)) << 4)),
+                           "r"(pack_bf16(o[e] * inv, o[e + 1] * inv)), "r"(pack_bf16(o[e + 2] * inv, o[e + 3] * inv)),
+                           "r"(pack_bf16(o[e + 4] * inv, o[e + 5] * inv)), "r"(pack_bf16(o[e + 6] * inv, o[e + 7] * inv))
+                           : "memory");
+            }
+            fin += (f4[0] + f4[1]) + (f4[2] + f4[3]);
+            __syncwarp();
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int rr = (lane >> 2) + 8 * x;
+              uint4 v;
+              asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                           : "r"(ostage + (uint32_t)(rr * 64 + (((lane & 3) ^ ((rr >> 1) & 3)) << 4))) : "memory");
+              if (q * 32 + rr < n_rows) *reinterpret_cast<uint4*>(ob + out_off[x]) = v;
+            }
+            __syncwarp();
           }
-          __syncwarp();
         }
+        odd |= row < n_rows && !(fin < INFINITY);
       }
       if (u.r.b < 0) break;
       ++n;
