@@ -100,7 +100,7 @@ __device__ __forceinline__ void quarter_sync(int q) { asm volatile("bar.sync %0,
 // logits in tensor memory at `sb`, the thread's are columns [64 g, 64 g + 64), visible those with a bit in `vis`; P = 2^(S - m)
 // goes over them as bf16 pairs, 32 columns per half.  m: running maximum (log2 units) of the row, l: sum over this thread's
 // columns, acc: the accumulator's rows of this warp.  `prev_done` returns once every P V so far has completed.  Without
-// `effect` nothing is written (a rehearsal of the code).  scale_log2: what a logit is multiplied by (queries that come scaled: log2(e)).
+// `effect` nothing is written (a rehearsal of the code).
 //
 // P of the two halves is published by half, and the product of the first 64 keys starts with the first half alone, over all
 // channels of the accumulator.  So the warps of a quarter, which rescale half of the channels each and take that branch
@@ -108,7 +108,7 @@ __device__ __forceinline__ void quarter_sync(int q) { asm volatile("bar.sync %0,
 constexpr float PAIR_RESCALE = 8.0f;          // log2 units by which a maximum grows before the accumulator is rescaled
 template <int DH, typename PrevDone>
 __device__ __forceinline__ void pair_softmax_tile(float& m, float& l, float (*xch)[128], uint32_t sb, uint32_t acc, int g, int q, int row, uint64_t vis,
-                                                  bool effect, PrevDone prev_done, const float scale_log2 = LOG2E) {
+                                                  bool effect, PrevDone prev_done) {
   float s[64];
   tmem_ld64(sb + (uint32_t)(g * 64), s);
   const uint32_t v0 = (uint32_t)vis, v1 = (uint32_t)(vis >> 32);
@@ -121,7 +121,7 @@ __device__ __forceinline__ void pair_softmax_tile(float& m, float& l, float (*xc
   for (int c = 0; c < 64; ++c) mx4[c & 3] = fmaxf(mx4[c & 3], s[c]);
   xch[g][row] = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
   quarter_sync(q);                            // (also: both halves of these S rows have been read -> P may overwrite them)
-  const float mx = fmaxf(xch[0][row], xch[1][row]) * scale_log2;
+  const float mx = fmaxf(xch[0][row], xch[1][row]) * LOG2E;
   // keep the old maximum unless the new one exceeds it by more than the threshold (exact algebra, no rescaling)
   float m_new = m;
   if (mx > m + PAIR_RESCALE || m == -INFINITY) m_new = fmaxf(m, mx);
@@ -135,7 +135,7 @@ __device__ __forceinline__ void pair_softmax_tile(float& m, float& l, float (*xc
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int c = c16 * 32 + 2 * e;
-      const float e0 = ex2_fast(fmaf(s[c], scale_log2, nsub)), e1 = ex2_fast(fmaf(s[c + 1], scale_log2, nsub));
+      const float e0 = ex2_fast(fmaf(s[c], LOG2E, nsub)), e1 = ex2_fast(fmaf(s[c + 1], LOG2E, nsub));
       rs4[e & 3] += e0 + e1;
       w[e] = pack_bf16(e0, e1);
     }

@@ -533,8 +533,8 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
     const int per = paged_pair_tokens(group), pairs = paged_pair_resident((int)c->head_dim);
     const long long full = (tokens + per - 1) / per > holders ? (tokens + per - 1) / per : holders;
     p.pair = 1, p.units = tokens / per + holders;
-    // key ranges: a pair for each, of at least 256 keys
-    long long ranges = pairs / (full * c->n_kv_heads);
+    // key ranges where there are fewer units than one and a half rounds of the pairs (the kernel cuts them to equal pieces)
+    long long ranges = 2 * full * c->n_kv_heads < 3ll * pairs ? (3ll * pairs + full * c->n_kv_heads - 1) / (full * c->n_kv_heads) : 1;
     if (ranges > keys / 256) ranges = keys / 256;
     p.ranges = (int)(ranges < 1 ? 1 : ranges > 64 ? 64 : ranges);
     return p;

@@ -3,8 +3,8 @@
 // A pair takes a unit: 2 x 128 packed rows (each CTA floor(128 / group) tokens of a request with the query heads of one kv head) and
 // walks the keys that any of them sees, then goes on to its next unit without leaving the pipeline: the next unit's operands are on their way
 // and its first logits go through the softmax while the accumulator of the last one is read out.
-//   S = Q K^T   M = 256, N = 128 keys, K = head_dim; Q and K in shared memory; two S buffers in tensor memory
-//   softmax     two threads per row (half of the columns each), straight from tensor memory; P (bf16) over the S buffer; the accumulator
+//   S = Q K^T   M = 256, N = 128 keys, K = head_dim; Q and K in shared memory; two S buffers (head_dim 128: three) in tensor memory
+//   softmax     four threads per row, straight from tensor memory; P (bf16) over the S buffer; the accumulator
 //               is rescaled only when a maximum grows by more than 2^8 (the old one is kept otherwise: exact algebra)
 //   O += P V    M = 256, N = head_dim, K = 128 keys; P is the tensor-memory A operand, V an MN-major B operand
 // K: CTA h of the pair fetches block h (64 keys) of a tile, V: its half of the channels of both blocks; the tensor cores read the other
@@ -16,7 +16,7 @@
 // rows whose result is not finite are looked at again after the last unit (see paged_row_alone).
 //
 // Few units (short chunks over long histories): a unit's keys are split over several pairs, the fp32 results are merged by k_paged_merge.
-// Warps of a CTA: 0 fetches K and Q, 1 V; 3 issues the MMAs (leader CTA); 4-11 softmax, correction, output.  Every wait is bounded; after
+// Warps of a CTA: 0 fetches K and Q, 1 V; 3 issues the MMAs (leader CTA); 4-19 softmax, correction, output.  Every wait is bounded; after
 // a give-up the protocol runs to its end and only the global stores are skipped.
 #include <cstdio>
 
@@ -29,8 +29,9 @@ namespace phyai {
 namespace {
 
 constexpr int KB = 128;                        // keys per tile: two blocks of 64
-constexpr int PP_THREADS = 12 * 32;
+constexpr int PP_THREADS = 20 * 32;
 constexpr int PAIR_LEAST = 2;                  // tiles of keys in a range, at least
+constexpr int PAIR_PIECES = 3;                 // ranges a pair takes where units are split
 
 template <int DH>
 struct PpLayout {
@@ -38,8 +39,9 @@ struct PpLayout {
   static constexpr int PIECE = (DH / 128) * KBLOCK;          // 64 keys x DH / 2 channels
   static constexpr int TILE = 2 * PIECE;                     // K: this CTA's block; V: both blocks, its channel half
   static constexpr int QTILE = 128 * DH * 2;
-  static constexpr int STG = 2048;                           // output staging of a warp: 32 rows x 32 columns
-  static constexpr size_t SMEM = 1024 + 4 * (size_t)TILE + QTILE + 8 * STG;
+  static constexpr int STG = 1024;                           // output staging of a warp: 32 rows x 16 columns
+  static constexpr int NB = (512 - DH) / 128;                // buffers of logits: what the accumulator leaves of the 512 columns
+  static constexpr size_t SMEM = 1024 + 2 * NB * (size_t)TILE + QTILE + 16 * STG;
 };
 
 __device__ __forceinline__ void copy4d(uint32_t dst, const CUtensorMap* map, int c1, int c2, int c3, uint32_t bar) {
@@ -76,6 +78,130 @@ __device__ __forceinline__ void umma2_ts_x4(uint32_t d, uint32_t ta, uint64_t db
       : "memory");
 }
 
+// ---- pairs of fp32 numbers in one instruction
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// Waits of the pipeline: one instruction in which the warp is suspended until the phase completes, and a call where that takes long.  (The bounded
+// polling loop inline at every wait is code, and code is time here: the warp that issues the MMAs shares its scheduler's instruction
+// cache with four softmax warps.)
+__device__ __noinline__ void wait_long(uint32_t bar, uint32_t parity, const WaitCtx* c) { mbar_wait_drain(bar, parity, *c); }
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, const WaitCtx& c) {
+  if (!mbar_try(bar, parity)) wait_long(bar, parity, &c);
+}
+__device__ __forceinline__ void wait_warp(uint32_t bar, uint32_t parity, const WaitCtx& c) {      // by a whole warp
+  wait(bar, parity, c);
+  __syncwarp();
+}
+// index of a buffer in a ring of N and the parity of its phase
+template <int N>
+struct Ring {
+  int at = 0;
+  uint32_t parity = 0;
+  __device__ __forceinline__ void next() {
+    if (++at == N) at = 0, parity ^= 1u;
+  }
+};
+
+// the four warps that share the rows of a tensor-memory lane quarter
+__device__ __forceinline__ void rows_sync(int q) { asm volatile("bar.sync %0, 128;" ::"r"(4 + q) : "memory"); }
+
+// Softmax of a tile of 128 keys, four threads per row (lane quarter q, column part g; 32 columns each, the first `vis` of which the row
+// sees; not `live`: a row of no token, whatever it holds): P = 2^(scale S - m) over the logits, as bf16 pairs, 16 columns per part.  m: running maximum (log2 units) of the row, l: sum over
+// this thread's columns, acc: the accumulator's rows of this warp, rescaled when the maximum grows; `prev_done` returns once every P V so far
+// has completed.  P is published by halves of the keys, and the product of the first 64 starts with the first half alone, over all channels: the
+// warps of a quarter, which rescale a fourth of the channels each, meet behind that.
+// The special-function unit (16 a clock and SM) takes 1024 clocks of a tile's 1700.  (A quarter or half of the powers by a polynomial on the FMA
+// pipe: 1.04 and 1.10 times the kernel's time; the instructions cost what the unit gains.)  A NaN or +infinity among the logits makes the
+// maximum and so the whole row NaN.
+template <int DH, typename PrevDone>
+__device__ __forceinline__ void softmax_tile(float& m, float& l, float (*xch)[128], uint32_t sb, uint32_t acc, int g, int q, int row, int vis, bool live, float scale,
+                                             PrevDone prev_done) {
+  float s[32];
+  tmem_ld32(sb + (uint32_t)(g * 32), s);
+  if (__any_sync(0xffffffffu, vis < 32)) {
+#pragma unroll
+    for (int c = 0; c < 32; ++c) s[c] = c < vis ? s[c] : -INFINITY;
+  }
+  float mx4[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+  for (int c = 4; c < 28; c += 8)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mx4[e] = max3_nan(mx4[e], s[c + e], s[c + 4 + e]);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) mx4[e] = max_nan(mx4[e], s[28 + e]);
+  xch[g][row] = max_nan(max3_nan(mx4[0], mx4[1], mx4[2]), mx4[3]);
+  rows_sync(q);                               // (also: all parts of these S rows have been read -> P may overwrite them)
+  float mx = max_nan(max3_nan(xch[0][row], xch[1][row], xch[2][row]), xch[3][row]) * scale;
+  mx = mx < INFINITY ? mx : NAN;
+  // keep the old maximum unless the new one exceeds it by more than the threshold (exact algebra, no rescaling)
+  float m_new = m;
+  if (!(mx <= m + PAIR_RESCALE) || m == -INFINITY) m_new = max_nan(m, mx);
+  const bool rescale = live && m_new != m && m != -INFINITY;
+  const float corr = rescale ? exp2f(m - m_new) : 1.0f;
+  const float nsub = m_new == -INFINITY ? 0.f : -m_new;
+  const uint64_t scale2 = pack2(scale, scale), nsub2 = pack2(nsub, nsub);
+  uint64_t rs[2] = {0, 0};
+  uint32_t w[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    uint64_t p = fma2(pack2(s[2 * e], s[2 * e + 1]), scale2, nsub2);
+    float e0, e1;
+    unpack2(p, e0, e1);
+    e0 = ex2_fast(e0), e1 = ex2_fast(e1);
+    rs[e & 1] = add2(rs[e & 1], pack2(e0, e1));
+    w[e] = pack_bf16(e0, e1);
+  }
+  tmem_st16u(sb + (uint32_t)(g * 16), w);
+  if (__any_sync(0xffffffffu, rescale)) {     // rare: rescale this warp's channels of its rows of the accumulator
+    prev_done();
+    __syncwarp();
+    tc_fence_after();
+#pragma unroll 1
+    for (int c = g * (DH / 4); c < (g + 1) * (DH / 4); c += 16) {
+      float o[16];
+      tmem_ld16(acc + (uint32_t)c, o);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[e] *= corr;
+      tmem_st16(acc + (uint32_t)c, o);
+    }
+    tmem_st_wait();
+    tc_fence_before();
+    rows_sync(q);
+    tc_fence_after();
+  }
+  tmem_st_wait();
+  tc_fence_before();
+  __syncwarp();
+  float a0, a1;
+  unpack2(add2(rs[0], rs[1]), a0, a1);
+  l = l * corr + (a0 + a1);
+  m = m_new;
+}
+
 struct Unit {
   PagedRequest r;      // r.b < 0: none
   int hk, tok0;        // first of the unit's tokens in the request
@@ -88,17 +214,19 @@ template <int DH>
 __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     k_paged_pair(const PagedAttn a, const __grid_constant__ CUtensorMap tmq, const __grid_constant__ CUtensorMap tmkv, const int piece_shift) {
   using L = PpLayout<DH>;
+  constexpr int NB = L::NB;
   constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(KB >> 3) << 17) | ((256u >> 4) << 24);
   constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((256u >> 4) << 24);
 
   extern __shared__ uint8_t smem_raw[];
   // leader: operands of a buffer complete in both CTAs, P of a buffer (by column half) complete in both, Q complete in both, accumulator
   // read out in both.  Each CTA: logits / P V complete, all logits of a unit complete; own V blocks that are cleared in part.
-  __shared__ __align__(8) uint64_t k_full[2], v_full[2], p_full[2][2], q_full, o_free, s_full[2], pv_done[2], q_free, v_own;
+  __shared__ __align__(8) uint64_t k_full[NB], v_full[NB], p_full[NB][2], q_full, o_free, s_full[NB], pv_done[NB], q_free, v_own;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, s_skip;
-  __shared__ float xch[2][2][128], xsum[2][2][128];       // what the two half-row threads of a row exchange: maximum (by tile parity), sum (by unit parity)
+  __shared__ float xch[2][4][128], xsum[2][4][128];       // what the four threads of a row exchange: maxima (by tile parity), sums (by unit parity)
   __shared__ int s_first[PAGED_MAX_BATCH + 1], s_warp[PP_THREADS / 32];
+  __shared__ long long s_sum[PP_THREADS / 32];
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int half = blockIdx.x & 1, pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
@@ -106,14 +234,14 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   if (tid == 32) prefetch_tmap(&tmkv), prefetch_tmap(&tmq);
 
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t Ks = base, Vs = base + 2 * L::TILE, Qs = base + 4 * L::TILE;
+  const uint32_t Ks = base, Vs = base + NB * L::TILE, Qs = base + 2 * NB * L::TILE;
   if (tid == 0) {
     abort_flag = 0;
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&k_full[i]), 1), mbar_init(smem_u32(&v_full[i]), 2), mbar_init(smem_u32(&p_full[i][0]), 8), mbar_init(smem_u32(&p_full[i][1]), 8);
+    for (int i = 0; i < NB; ++i) {
+      mbar_init(smem_u32(&k_full[i]), 1), mbar_init(smem_u32(&v_full[i]), 2), mbar_init(smem_u32(&p_full[i][0]), 16), mbar_init(smem_u32(&p_full[i][1]), 16);
       mbar_init(smem_u32(&s_full[i]), 1), mbar_init(smem_u32(&pv_done[i]), 1);
     }
-    mbar_init(smem_u32(&q_full), 1), mbar_init(smem_u32(&o_free), 16), mbar_init(smem_u32(&q_free), 1), mbar_init(smem_u32(&v_own), 1);
+    mbar_init(smem_u32(&q_full), 1), mbar_init(smem_u32(&o_free), 32), mbar_init(smem_u32(&q_free), 1), mbar_init(smem_u32(&v_own), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 3) {
@@ -125,7 +253,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   tc_fence_after();
   pdl_launch_dependents();                          // (not before: a later kernel must not take tensor memory that this one still waits for)
   const uint32_t tmem_base = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&tmem_slot), 0);
-  const uint32_t tmem_s = tmem_base, tmem_o = tmem_base + 2 * KB;
+  const uint32_t tmem_s = tmem_base, tmem_o = tmem_base + NB * KB;
   const WaitCtx wc{a.status, &abort_flag, a.wait_limit}, wl{a.status, &abort_flag, a.wait_limit, true};
 
   // ---- units before each request (both CTAs of a pair read the same lengths and come to the same list)
@@ -133,14 +261,17 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   if (tid == 0) s_skip = status_set(a.status), s_first[0] = 0;
   bool bad = false;
   int acc = 0;
+  long long tiles_all = 0;                          // of whole requests' units: at least what the units have
   for (int i0 = 0; i0 < a.pb.batch; i0 += PP_THREADS) {
     const int i = i0 + tid;
     int n = 0;
     if (i < a.pb.batch) {
       const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1];
-      const bool b = paged_entry_bad(a.pb, i, lo, hi, a.pb.kv_lens[i], false);
+      const int kv = a.pb.kv_lens[i];
+      const bool b = paged_entry_bad(a.pb, i, lo, hi, kv, false);
       bad |= b;
       n = b ? 0 : (hi - lo + 2 * TOK - 1) / (2 * TOK);
+      tiles_all += (long long)n * ((kv + KB - 1) / KB);
     }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -161,6 +292,17 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   if (bad && tid == 0) atomicExch(a.status, ST_INVALID_ARG);
   const bool skip = s_skip != 0;
   const int n_units = bad ? 0 : acc * a.hkv * a.ranges;
+  int least = PAIR_LEAST;
+  if (a.ranges > 1) {                               // tiles of a range: three ranges a pair
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) tiles_all += __shfl_xor_sync(0xffffffffu, tiles_all, o);
+    if (lane == 0) s_sum[warp] = tiles_all;
+    __syncthreads();
+    tiles_all = 0;
+    for (int w = 0; w < PP_THREADS / 32; ++w) tiles_all += s_sum[w];
+    const long long per = tiles_all * a.hkv / (PAIR_PIECES * n_pairs);
+    least = (int)(per < PAIR_LEAST ? PAIR_LEAST : per > 0x7fffffff ? 0x7fffffff : per);
+  }
 
   // Units of this pair: of every round of n_pairs units one, rounds dealt back and forth (a request's last, longest tiles come first).
   auto index_of = [&](int k) { return k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair); };
@@ -179,7 +321,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     u.r.prefix = a.prefix_lens ? min(max(a.prefix_lens[lo], 0), u.r.kv) : 0;
     u.tok0 = (s_first[lo + 1] - 1 - ut) * 2 * TOK;
     const int keys = u.r.limit(min(u.tok0 + 2 * TOK, u.r.n) - 1, a.causal), tiles = max(1, (keys + KB - 1) / KB);
-    u.ranges = ranges_of(tiles, a.ranges, PAIR_LEAST);
+    u.ranges = ranges_of(tiles, a.ranges, least);
     u.t0 = u.range < u.ranges ? (int)((long long)tiles * u.range / u.ranges) : 0;
     u.T = u.range < u.ranges ? (int)((long long)tiles * (u.range + 1) / u.ranges) - u.t0 : 0;
     return u;
@@ -212,22 +354,23 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   const uint32_t piece_bytes = (uint32_t)(128 << piece_shift);
 
   if (warp == 0) {
-    // =========================== K: a buffer is free again once the logits of the tile two before exist ==================
+    // =========================== K: a buffer is free again once the logits of the tile NB before exist ==================
     const int nc = np * (DH / 64 / cb), pc = lane % np, ch = (lane / np) * cb;        // copies of a block: one per lane
     int k = 0, n = 0, i = 0;
+    Ring<NB> rg;
     Unit u = next_unit(k);
     while (u.r.b >= 0) {
-      for (int t = 0; t < u.T; ++t, ++n) {
+      for (int t = 0; t < u.T; ++t, ++n, rg.next()) {
         const int row = lane < nc ? row_of(u.r, (u.t0 + t) * KB + half * 64 + (pc << piece_shift)) : 0;
-        if (n >= 2 && lane == 0) mbar_wait_drain(smem_u32(&s_full[n & 1]), (uint32_t)((n - 2) >> 1) & 1u, wl);
-        __syncwarp();
-        const uint32_t bar = smem_u32(&k_full[n & 1]), dst = Ks + (uint32_t)(n & 1) * L::TILE;
+        const int bf = rg.at;
+        if (n >= NB) wait_warp(smem_u32(&s_full[bf]), rg.parity ^ 1u, wl);
+        const uint32_t bar = smem_u32(&k_full[bf]), dst = Ks + (uint32_t)bf * L::TILE;
         if (half == 0 && lane == 0) mbar_expect_tx(bar, (uint32_t)L::TILE * 2);
         __syncwarp();
         if (lane < nc) copy4d(dst + (uint32_t)ch * L::KBLOCK + (uint32_t)pc * piece_bytes, &tmkv, row, u.hk * (DH / 64) + ch, a.plane, bar & LEADER_MASK);
         if (t == 0) {                             // Q: its tile is free again once the last logits of the unit before exist
           if (lane == 0) {
-            if (i > 0) mbar_wait_drain(smem_u32(&q_free), (uint32_t)(i - 1) & 1u, wl);
+            if (i > 0) wait(smem_u32(&q_free), (uint32_t)(i - 1) & 1u, wl);
             if (half == 0) mbar_expect_tx(smem_u32(&q_full), 2 * (uint32_t)(TOK * G * DH * 2));
           }
           __syncwarp();
@@ -240,26 +383,28 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     }
     __syncwarp();
   } else if (warp == 1) {
-    // =========================== V: a buffer is free again once P V of the tile two before has completed ==================
+    // =========================== V: a buffer is free again once P V of the tile NB before has completed ==================
     const uint32_t full_lead = map_rank(smem_u32(&v_full[0]), 0);
     const int nb = np * (DH / 128 / cb), blk = lane / nb, pc = lane % np, ch = ((lane % nb) / np) * cb;   // copies of a block; block of this lane
     uint32_t ph_own = 0;
     int k = 0, n = 0;
+    Ring<NB> rg;
     Unit u = next_unit(k);
     while (u.r.b >= 0) {
-      for (int t = 0; t < u.T; ++t, ++n) {
+      for (int t = 0; t < u.T; ++t, ++n, rg.next()) {
         const int key0 = (u.t0 + t) * KB, rem = u.r.kv - key0;                        // rows past the cached tokens: rem .. of the tile
         // (rows up to the end of the piece that they begin in; later pieces are zeros)
         const int clear_to = (rem + (1 << piece_shift) - 1) >> piece_shift << piece_shift;
         const bool clear = rem > 0 && rem < KB && clear_to > rem;
         const int row = lane < 2 * nb ? row_of(u.r, key0 + blk * 64 + (pc << piece_shift)) : 0;
-        const uint32_t dst = Vs + (uint32_t)(n & 1) * L::TILE;
-        uint32_t bar = smem_u32(&v_full[n & 1]);
+        const int bf = rg.at;
+        const uint32_t dst = Vs + (uint32_t)bf * L::TILE;
+        uint32_t bar = smem_u32(&v_full[bf]);
         if (lane == 0) {
-          if (n >= 2) mbar_wait_drain(smem_u32(&pv_done[n & 1]), (uint32_t)((n - 2) >> 1) & 1u, wl);
+          if (n >= NB) wait(smem_u32(&pv_done[bf]), rg.parity ^ 1u, wl);
           if (clear) mbar_expect_tx(smem_u32(&v_own), (uint32_t)L::TILE);
           else if (half == 0) mbar_expect_tx(bar, 2 * (uint32_t)L::TILE);
-          else remote_arrive(full_lead + (uint32_t)(n & 1) * 8u);
+          else remote_arrive(full_lead + (uint32_t)bf * 8u);
         }
         __syncwarp();
         bar = clear ? smem_u32(&v_own) : bar & LEADER_MASK;
@@ -267,7 +412,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
           copy4d(dst + (uint32_t)blk * L::PIECE + (uint32_t)ch * L::KBLOCK + (uint32_t)pc * piece_bytes, &tmkv, row, u.hk * (DH / 64) + half * (DH / 128) + ch,
                  a.plane + 1, bar);
         if (clear) {
-          mbar_wait_drain(bar, ph_own, wl);
+          wait_warp(bar, ph_own, wl);
           ph_own ^= 1u;
           for (int i = lane; i < (clear_to - rem) * (DH / 16); i += 32) {              // (a row: 8 x 16 bytes in each of DH / 128 blocks)
             const int r = rem + i / (DH / 16), c = i % (DH / 16);
@@ -275,188 +420,177 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
           }
           fence_async_smem();                    // generic-proxy writes, read next by the tensor cores
           __syncwarp();
-          if (lane == 0) remote_arrive_stores(full_lead + (uint32_t)(n & 1) * 8u);
+          if (lane == 0) remote_arrive_stores(full_lead + (uint32_t)bf * 8u);
         }
       }
       u = next_unit(k);
     }
     __syncwarp();
   } else if (warp == 3) {
-    // =========================== MMA issuer (leader CTA): S(0), S(1), then P(n) V(n), S(n + 2), across the units ==========
-    // The products wait for one another through what stands between their MMAs: S(n + 2) follows P(n) V(n), whose P is in its buffer, in the
+    // =========================== MMA issuer (leader CTA): S(0) .. S(NB - 1), then P(n) V(n), S(n + NB), across the units ==========
+    // The products wait for one another through what stands between their MMAs: S(n + NB) follows P(n) V(n), whose P is in its buffer, in the
     // pipe's order.  So the loop is short: plain waits in a fixed order, one election, four MMAs a statement.  (Whichever of the two had its
     // operands first, an election per MMA: 600 to 900 clocks from the last MMA of a product to the first of the next, beside two busy warps of
-    // the scheduler, 3400 per tile.  Two warps, one per product: 2770, as S(n + 2) then waits for the completion of P(n) V(n).)
+    // the scheduler, 3400 per tile.  Two warps, one per product: 2770, as S(n + NB) then waits for the completion of P(n) V(n).)
     if (half == 0) {
       const uint32_t elected = elect_one() ? 1u : 0u;
-      int k = 0, ns = 0, is = 0, ts = 0;                          // logits: tile of the call, unit, tile of the unit
+      int k = 0, ahead = 0, ts = 0, kp = 0;                       // ahead: logits issued whose P V has not been; ts: tile of the unit
+      uint32_t par_q = 0, par_o = 1;
+      Ring<NB> rs, rp;
       Unit us = next_unit(k);
+      const uint64_t dq = make_desc(Qs);
       auto logits = [&] {
-        mbar_wait_drain(smem_u32(&k_full[ns & 1]), (uint32_t)(ns >> 1) & 1u, wc);
-        if (ts == 0) mbar_wait_drain(smem_u32(&q_full), (uint32_t)is & 1u, wc);
+        wait_warp(smem_u32(&k_full[rs.at]), rs.parity, wc);
+        if (ts == 0) wait_warp(smem_u32(&q_full), par_q, wc);
         tc_fence_after();
-        const uint64_t da = make_desc(Qs), db = make_desc(Ks + (uint32_t)(ns & 1) * L::TILE);      // (a 64-channel block further: 128 x 128 and 64 x 128 bytes)
+        const uint64_t db = make_desc(Ks + (uint32_t)rs.at * L::TILE);      // (a 64-channel block further: 128 x 128 and 64 x 128 bytes)
 #pragma unroll
         for (int c = 0; c < DH / 64; ++c)
-          umma2_ss_x4(tmem_s + (uint32_t)(ns & 1) * KB, da + (uint64_t)(c * ((128 * 128) >> 4)), db + (uint64_t)(c * (L::KBLOCK >> 4)), IDESC_S, c == 0 ? 1u : 0u, elected);
-        if (elected) umma2_commit(smem_u32(&s_full[ns & 1]));
-        ++ns;
+          umma2_ss_x4(tmem_s + (uint32_t)rs.at * KB, dq + (uint64_t)(c * ((128 * 128) >> 4)), db + (uint64_t)(c * (L::KBLOCK >> 4)), IDESC_S, c == 0 ? 1u : 0u, elected);
+        if (elected) umma2_commit(smem_u32(&s_full[rs.at]));
+        rs.next(), ++ahead;
         if (++ts == us.T) {
           if (elected) umma2_commit(smem_u32(&q_free));
-          ts = 0, ++is, us = next_unit(k);
+          ts = 0, par_q ^= 1u, us = next_unit(k);
         }
-        __syncwarp();
       };
-      int kp = 0;
-      Unit u = next_unit(kp);
-      if (us.r.b >= 0) logits();
-      for (int n = 0, i = 0; u.r.b >= 0; ++i) {
-        for (int t = 0; t < u.T; ++t, ++n) {
-          if (us.r.b >= 0) logits();                              // S(n + 1)
-          const uint32_t pf = smem_u32(&p_full[n & 1][0]), par = (uint32_t)(n >> 1) & 1u, vb = Vs + (uint32_t)(n & 1) * L::TILE;
-          mbar_wait_drain(smem_u32(&v_full[n & 1]), par, wc);
+      int i = 0;
+      for (Unit u = next_unit(kp); u.r.b >= 0; u = next_unit(kp), par_o ^= 1u, ++i) {
+        for (int t = 0; t < u.T; ++t, rp.next()) {
+          // Logits as far ahead as there are buffers; those of the next unit only once its queries are there, or nothing else is left
+          while (us.r.b >= 0 && ahead < NB && (ts > 0 || ahead == 0 || __all_sync(0xffffffffu, mbar_test(smem_u32(&q_full), par_q)))) logits();
+          const uint32_t pf = smem_u32(&p_full[rp.at][0]), vb = Vs + (uint32_t)rp.at * L::TILE;
+          wait_warp(smem_u32(&v_full[rp.at]), rp.parity, wc);
           // (the tile in which the cached tokens end: rows of it were cleared by a warp of each CTA)
-          if (u.r.kv < (u.t0 + t + 1) * KB) pair_acquire(smem_u32(&v_full[n & 1]), par);
-          if (t == 0 && i > 0) mbar_wait_drain(smem_u32(&o_free), (uint32_t)(i - 1) & 1u, wc);
+          if (u.r.kv < (u.t0 + t + 1) * KB) pair_acquire(smem_u32(&v_full[rp.at]), rp.parity);
+          if (t == 0 && i > 0) wait_warp(smem_u32(&o_free), par_o, wc);
 #pragma unroll
           for (int kh = 0; kh < 2; ++kh) {
-            mbar_wait_drain(pf + 8u * kh, par, wc);
+            wait_warp(pf + 8u * kh, rp.parity, wc);
             tc_fence_after();
             // A = P of this tile: bf16 pairs in the first 64 columns of its S buffer
-            umma2_ts_x4(tmem_o, tmem_s + (uint32_t)(n & 1) * KB + (uint32_t)kh * 32, make_desc_mn(vb + (uint32_t)kh * L::PIECE, L::KBLOCK, 1024), IDESC_PV,
+            umma2_ts_x4(tmem_o, tmem_s + (uint32_t)rp.at * KB + (uint32_t)kh * 32, make_desc_mn(vb + (uint32_t)kh * L::PIECE, L::KBLOCK, 1024), IDESC_PV,
                         t == 0 && kh == 0 ? 1u : 0u, elected);
           }
-          if (elected) umma2_commit(smem_u32(&pv_done[n & 1]));
-          __syncwarp();
+          if (elected) umma2_commit(smem_u32(&pv_done[rp.at]));
+          --ahead;
         }
-        u = next_unit(kp);
       }
     }
     __syncwarp();
   } else if (warp >= 4) {
     // =========================== softmax / correction / output ==============================================================
-    const int g = (warp - 4) >> 2;            // which half of a row's columns: block g of a tile
+    const int g = (warp - 4) >> 2;            // part of a row's columns
     const int q = warp & 3;
     const int row = q * 32 + lane;            // accumulator row = tensor-memory lane
     const int row_tok = row / G;              // token of the CTA's TOK (rows past TOK * G: none)
     const uint32_t lane_addr = (uint32_t)(q * 32) << 16;
-    const uint32_t pfull0 = map_rank(smem_u32(&p_full[0][g]), 0), ofree0 = map_rank(smem_u32(&o_free), 0);
+    const uint32_t pfull0 = map_rank(smem_u32(&p_full[0][g >> 1]), 0), ofree0 = map_rank(smem_u32(&o_free), 0);
     const uint32_t ostage = Qs + L::QTILE + (uint32_t)(warp - 4) * L::STG;
-    const int c0 = g * (DH / 2);              // first of this warp's output channels
-    float m = -INFINITY, l = 0.f, m_prev = 0.f, l_prev = 0.f;             // running maximum (log2 units) and sum (of this thread's columns)
-    int out_off[4];                           // where this lane stores of a unit's rows (lane / 4 + 8 x of the warp's 32)
+    const int c0 = g * (DH / 4);              // first of this warp's output channels
+    int out_off[2];                           // where this lane stores of a unit's rows (lane / 2 + 16 x of the warp's 32)
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int r = q * 32 + (lane >> 2) + 8 * x, rt = r / G;
-      out_off[x] = (rt * a.hq + r - rt * G) * DH + (lane & 3) * 8;
+    for (int x = 0; x < 2; ++x) {
+      const int r = q * 32 + (lane >> 1) + 16 * x, rt = r / G;
+      out_off[x] = (rt * a.hq + r - rt * G) * DH + c0 + (lane & 1) * 8;
     }
     bool odd = false;
     int k = 0, n = 0, i = 0;
-    Unit u = next_unit(k), prev = u;
-    int t = 0;
-    for (;;) {
-      if (u.r.b >= 0) {
-        const uint32_t sb = tmem_s + (uint32_t)(n & 1) * KB + lane_addr;
-        const int tok = u.tok0 + half * TOK + row_tok;
-        const int lim = row < TOK * G && tok < u.r.n ? u.r.limit(tok, a.causal) : 0;
-        const uint64_t vis = first_columns(lim - ((u.t0 + t) * KB + g * 64));
-        if (lane == 0) mbar_wait_drain(smem_u32(&s_full[n & 1]), (uint32_t)(n >> 1) & 1u, wc);
-        __syncwarp();
+    Ring<NB> rg;
+    uint32_t last_bar = 0, last_par = 0;      // of the tile before: its P V complete
+    Unit u = next_unit(k);
+    for (; u.r.b >= 0; ++i) {
+      const Unit me = u;
+      const int tok = me.tok0 + half * TOK + row_tok;
+      const bool live = row < TOK * G && tok < me.r.n;
+      // (rows of no token count as seeing all: masked, they would keep their warps in the masked form of every tile)
+      const int lim = live ? me.r.limit(tok, a.causal) - me.t0 * KB - g * 32 : 0x40000000;
+      float m = -INFINITY, l = 0.f;           // running maximum (log2 units) and sum (of this thread's columns)
+      for (int t = 0; t < me.T; ++t, ++n, rg.next()) {
+        wait_warp(smem_u32(&s_full[rg.at]), rg.parity, wc);
         tc_fence_after();
-        pair_softmax_tile<DH>(m, l, xch[n & 1], sb, tmem_o + lane_addr, g, q, row, vis, true, [&] {
-          if (lane == 0) mbar_wait_drain(smem_u32(&pv_done[(n - 1) & 1]), (uint32_t)((n - 1) >> 1) & 1u, wc);
-        }, a.scale_log2);
-        if (lane == 0) remote_arrive(pfull0 + (uint32_t)(n & 1) * 16u);
+        softmax_tile<DH>(m, l, xch[n & 1], tmem_s + (uint32_t)rg.at * KB + lane_addr, tmem_o + lane_addr, g, q, row, live ? lim - t * KB : KB, live, a.scale_log2,
+                         [&] { wait_warp(last_bar, last_par, wc); });
+        if (lane == 0) remote_arrive(pfull0 + (uint32_t)rg.at * 16u);
+        last_bar = smem_u32(&pv_done[rg.at]), last_par = rg.parity;
       }
-      if (t == 0 && i > 0) {
-        // ---- the unit before: O / l -> bf16, 32 columns at a time through a staging block of the warp, out with coalesced stores; or the
-        // accumulator of a key range as it is
-        xsum[i & 1][g][row] = l_prev;
-        quarter_sync(q);
-        const float sum = xsum[i & 1][0][row] + xsum[i & 1][1][row];
-        const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
-        if (lane == 0) mbar_wait_drain(smem_u32(&pv_done[(n - 1) & 1]), (uint32_t)((n - 1) >> 1) & 1u, wc);
-        __syncwarp();
-        tc_fence_after();
-        const bool okf = !skip && !*reinterpret_cast<volatile int*>(&abort_flag);
-        const int first_tok = prev.r.lo + prev.tok0 + half * TOK, n_rows = okf ? min(TOK, prev.r.n - prev.tok0 - half * TOK) * G : 0;
-        float fin = 0.f;
-        if (prev.ranges > 1) {
-          const size_t slot = ((size_t)prev.range * a.pb.tokens + first_tok + row_tok) * a.hq + prev.hk * G + (row - row_tok * G);
-          if (g == 0 && row < n_rows) a.part_ml[slot] = make_float4(m_prev, sum, (float)prev.ranges, 0.f);
+      u = next_unit(k);                       // (the next one, while the last product runs)
+      // ---- output: O / l -> bf16, 16 columns at a time through a staging block of the warp, out in whole sectors; or the accumulator
+      // of a key range as it is.  A rolled loop: run once per unit, its code comes from far at about 11 clocks an instruction.
+      xsum[i & 1][g][row] = l;
+      rows_sync(q);
+      const float sum = (xsum[i & 1][0][row] + xsum[i & 1][1][row]) + (xsum[i & 1][2][row] + xsum[i & 1][3][row]);
+      const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+      wait_warp(last_bar, last_par, wc);
+      tc_fence_after();
+      const bool okf = !skip && !*reinterpret_cast<volatile int*>(&abort_flag);
+      const int first_tok = me.r.lo + me.tok0 + half * TOK, n_rows = okf ? min(TOK, me.r.n - me.tok0 - half * TOK) * G : 0;
+      const bool whole = me.ranges == 1;
+      const size_t slot = ((size_t)me.range * a.pb.tokens + first_tok + row_tok) * a.hq + me.hk * G + (row - row_tok * G);
+      if (g == 0 && a.ranges > 1 && row < n_rows) a.part_ml[slot] = make_float4(m, sum, (float)me.ranges, 0.f);
+      __nv_bfloat16* ob = (__nv_bfloat16*)a.out + ((size_t)first_tok * a.hq + me.hk * G) * DH;
+      const uint64_t inv2 = pack2(inv, inv);
+      uint64_t fin2 = 0;
 #pragma unroll 1
-          for (int c = 0; c < DH / 2; c += 32) {
-            float o[32];
-            tmem_ld32(tmem_o + lane_addr + (uint32_t)(c0 + c), o);
-            if (row < n_rows) {
-              float* p = a.part_o + slot * DH + c0 + c;
-#pragma unroll
-              for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-            }
-#pragma unroll
-            for (int e = 0; e < 32; ++e) fin += fabsf(o[e]);
-          }
+      for (int c = 0; c < DH / 4; c += 16, ob += 16) {
+        float o[16];
+        tmem_ld16(tmem_o + lane_addr + (uint32_t)(c0 + c), o);
+        if (c + 16 == DH / 4) {               // the accumulator may be overwritten
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) remote_arrive(ofree0);     // the accumulator may be overwritten
-        } else {
-          if (g == 0 && a.ranges > 1 && row < n_rows)
-            a.part_ml[((size_t)first_tok + row_tok) * a.hq + prev.hk * G + (row - row_tok * G)] = make_float4(m_prev, sum, 1.f, 0.f);
-          __nv_bfloat16* ob = (__nv_bfloat16*)a.out + ((size_t)first_tok * a.hq + prev.hk * G) * DH + c0;
-          const uint32_t rowp = ostage + (uint32_t)lane * 64u;
-          // (a rolled loop: run once per unit, its code comes from far at about 11 clocks an instruction; unrolled it took 5000 clocks)
-#pragma unroll 1
-          for (int c = 0; c < DH / 2; c += 32, ob += 32) {
-            float o[32], f4[4] = {0.f, 0.f, 0.f, 0.f};
-            tmem_ld32(tmem_o + lane_addr + (uint32_t)(c0 + c), o);
-            if (c + 32 == DH / 2) {                   // the accumulator may be overwritten
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) remote_arrive(ofree0);
-            }
-#pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) f4[j & 3] += fabsf(o[e + j]);
-              asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(rowp + (uint32_t)(((e >> 3) ^ ((lane >> 1) & 3)) << 4)),
-                           "r"(pack_bf16(o[e] * inv, o[e + 1] * inv)), "r"(pack_bf16(o[e + 2] * inv, o[e + 3] * inv)),
-                           "r"(pack_bf16(o[e + 4] * inv, o[e + 5] * inv)), "r"(pack_bf16(o[e + 6] * inv, o[e + 7] * inv))
-                           : "memory");
-            }
-            fin += (f4[0] + f4[1]) + (f4[2] + f4[3]);
-            __syncwarp();
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const int rr = (lane >> 2) + 8 * x;
-              uint4 v;
-              asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                           : "r"(ostage + (uint32_t)(rr * 64 + (((lane & 3) ^ ((rr >> 1) & 3)) << 4))) : "memory");
-              if (q * 32 + rr < n_rows) *reinterpret_cast<uint4*>(ob + out_off[x]) = v;
-            }
-            __syncwarp();
-          }
+          if (lane == 0) remote_arrive(ofree0);
         }
-        odd |= row < n_rows && !(fin < INFINITY);
+        if (!whole) {
+          if (row < n_rows) {
+            float* p = a.part_o + slot * DH + c0 + c;
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          }
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) fin2 = fma2(pack2(o[e], o[e + 1]), 0ull, fin2);
+          continue;
+        }
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint64_t o2 = pack2(o[2 * e], o[2 * e + 1]);
+          float e0, e1;
+          fin2 = fma2(o2, 0ull, fin2);        // (NaN of an infinity or a NaN)
+          unpack2(fma2(o2, inv2, 0ull), e0, e1);
+          w[e] = pack_bf16(e0, e1);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(ostage + (uint32_t)(lane * 32 + ((e ^ ((lane >> 2) & 1)) << 4))), "r"(w[4 * e]), "r"(w[4 * e + 1]),
+                       "r"(w[4 * e + 2]), "r"(w[4 * e + 3])
+                       : "memory");
+        __syncwarp();
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int rr = (lane >> 1) + 16 * x;
+          uint4 v;
+          asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                       : "r"(ostage + (uint32_t)(rr * 32 + (((lane & 1) ^ ((rr >> 2) & 1)) << 4))) : "memory");
+          if (q * 32 + rr < n_rows) *reinterpret_cast<uint4*>(ob + out_off[x]) = v;
+        }
+        __syncwarp();
       }
-      if (u.r.b < 0) break;
-      ++n;
-      if (++t == u.T) {
-        l_prev = l, m_prev = m, m = -INFINITY, l = 0.f;
-        prev = u, t = 0, ++i, u = next_unit(k);
-      }
+      float f0, f1;
+      unpack2(fin2, f0, f1);
+      odd |= row < n_rows && !(f0 + f1 == 0.f);
     }
     // ---- rows that are not finite although the values that they see may be: those of them with an infinity or a NaN among the keys of
     // their tiles that they do not see once more, key by key (channel by channel right otherwise: an infinite value is of one channel)
     if (a.causal) {
       __threadfence();
-      quarter_sync(q);                      // (maxima beside a range's result: written by the other warp of the quarter)
+      rows_sync(q);                           // (maxima beside a range's result: written by another warp of the quarter)
     }
     if (a.causal && __any_sync(0xffffffffu, odd) && !*reinterpret_cast<volatile int*>(&abort_flag)) {
       k = 0;
       for (u = next_unit(k); u.r.b >= 0; u = next_unit(k)) {
         const int n_rows = min(TOK, u.r.n - u.tok0 - half * TOK) * G, end = min((u.t0 + u.T) * KB, u.r.kv);
         for (int rr = q * 32; rr < min(n_rows, q * 32 + 32); ++rr) {
-          constexpr int C = DH / 64;
+          constexpr int C = DH / 128;         // channels of a lane, of this warp's
           const int rt = rr / G, tok = u.r.lo + u.tok0 + half * TOK + rt, head = u.hk * G + rr - rt * G;
           const int lim = u.r.limit(u.tok0 + half * TOK + rt, 1);
           const size_t slot = ((size_t)u.range * a.pb.tokens + tok) * a.hq + head;
@@ -473,7 +607,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
 #pragma unroll
           for (int e = 0; e < DH / 32; ++e) {
             const int c = lane * (DH / 32) + e - c0;
-            if (c < 0 || c >= DH / 2) continue;
+            if (c < 0 || c >= DH / 4) continue;
             if (u.ranges == 1) ob[c] = __float2bfloat16_rn(o[e] * w);
             else of[c] = o[e] * w;
           }
