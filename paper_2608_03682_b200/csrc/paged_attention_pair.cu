@@ -16,7 +16,7 @@
 // rows whose result is not finite are looked at again after the last unit (see paged_row_alone).
 //
 // Few units (short chunks over long histories): a unit's keys are split over several pairs, the fp32 results are merged by k_paged_merge.
-// Warps of a CTA: 0 fetches K and Q, 1 V; 3 issues the MMAs (leader CTA); 4-19 softmax, correction, output.  Every wait is bounded; after
+// Warps of a CTA: 0 fetches K and Q, 1 V; 2 goes through the units; 3 issues the MMAs (leader CTA); 4-19 softmax, correction, output.  Every wait is bounded; after
 // a give-up the protocol runs to its end and only the global stores are skipped.
 #include <cstdio>
 
@@ -78,23 +78,6 @@ __device__ __forceinline__ void umma2_ts_x4(uint32_t d, uint32_t ta, uint64_t db
       : "memory");
 }
 
-// ---- pairs of fp32 numbers in one instruction
-__device__ __forceinline__ uint64_t pack2(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -143,6 +126,7 @@ __device__ __forceinline__ void softmax_tile(float& m, float& l, float (*xch)[12
   float s[32];
   tmem_ld32(sb + (uint32_t)(g * 32), s);
   if (__any_sync(0xffffffffu, vis < 32)) {
+    asm volatile("" ::: "memory");            // (a branch: as selects, the instructions below would be issued for every tile)
 #pragma unroll
     for (int c = 0; c < 32; ++c) s[c] = c < vis ? s[c] : -INFINITY;
   }
@@ -163,16 +147,12 @@ __device__ __forceinline__ void softmax_tile(float& m, float& l, float (*xch)[12
   const bool rescale = live && m_new != m && m != -INFINITY;
   const float corr = rescale ? exp2f(m - m_new) : 1.0f;
   const float nsub = m_new == -INFINITY ? 0.f : -m_new;
-  const uint64_t scale2 = pack2(scale, scale), nsub2 = pack2(nsub, nsub);
-  uint64_t rs[2] = {0, 0};
+  float rs[4] = {0.f, 0.f, 0.f, 0.f};
   uint32_t w[16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
-    uint64_t p = fma2(pack2(s[2 * e], s[2 * e + 1]), scale2, nsub2);
-    float e0, e1;
-    unpack2(p, e0, e1);
-    e0 = ex2_fast(e0), e1 = ex2_fast(e1);
-    rs[e & 1] = add2(rs[e & 1], pack2(e0, e1));
+    const float e0 = ex2_fast(fmaf(s[2 * e], scale, nsub)), e1 = ex2_fast(fmaf(s[2 * e + 1], scale, nsub));
+    rs[e & 1] += e0, rs[2 + (e & 1)] += e1;
     w[e] = pack_bf16(e0, e1);
   }
   tmem_st16u(sb + (uint32_t)(g * 16), w);
@@ -196,19 +176,18 @@ __device__ __forceinline__ void softmax_tile(float& m, float& l, float (*xch)[12
   tmem_st_wait();
   tc_fence_before();
   __syncwarp();
-  float a0, a1;
-  unpack2(add2(rs[0], rs[1]), a0, a1);
-  l = l * corr + (a0 + a1);
+  l = l * corr + ((rs[0] + rs[1]) + (rs[2] + rs[3]));
   m = m_new;
 }
 
-struct Unit {
+struct alignas(16) Unit {
   PagedRequest r;      // r.b < 0: none
   int hk, tok0;        // first of the unit's tokens in the request
   int t0, T;           // tiles of 128 keys: first, how many (one at least: without a key all of it is masked)
   int range, ranges;
-  int index;           // of the call's units x kv heads x ranges
+  int pad;
 };
+constexpr int UNITS = 8;                       // units that the scheduling warp is ahead, at most
 
 template <int DH>
 __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
@@ -221,7 +200,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   extern __shared__ uint8_t smem_raw[];
   // leader: operands of a buffer complete in both CTAs, P of a buffer (by column half) complete in both, Q complete in both, accumulator
   // read out in both.  Each CTA: logits / P V complete, all logits of a unit complete; own V blocks that are cleared in part.
-  __shared__ __align__(8) uint64_t k_full[NB], v_full[NB], p_full[NB][2], q_full, o_free, s_full[NB], pv_done[NB], q_free, v_own;
+  __shared__ __align__(8) uint64_t k_full[NB], v_full[NB], p_full[NB][2], q_full, o_free, s_full[NB], pv_done[NB], q_free, v_own, u_full[UNITS], u_free[UNITS];
+  __shared__ Unit s_unit[UNITS];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, s_skip;
   __shared__ float xch[2][4][128], xsum[2][4][128];       // what the four threads of a row exchange: maxima (by tile parity), sums (by unit parity)
@@ -241,6 +221,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
       mbar_init(smem_u32(&k_full[i]), 1), mbar_init(smem_u32(&v_full[i]), 2), mbar_init(smem_u32(&p_full[i][0]), 16), mbar_init(smem_u32(&p_full[i][1]), 16);
       mbar_init(smem_u32(&s_full[i]), 1), mbar_init(smem_u32(&pv_done[i]), 1);
     }
+    for (int i = 0; i < UNITS; ++i) mbar_init(smem_u32(&u_full[i]), 1), mbar_init(smem_u32(&u_free[i]), half == 0 ? 19 : 18);
     mbar_init(smem_u32(&q_full), 1), mbar_init(smem_u32(&o_free), 32), mbar_init(smem_u32(&q_free), 1), mbar_init(smem_u32(&v_own), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -254,7 +235,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   pdl_launch_dependents();                          // (not before: a later kernel must not take tensor memory that this one still waits for)
   const uint32_t tmem_base = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&tmem_slot), 0);
   const uint32_t tmem_s = tmem_base, tmem_o = tmem_base + NB * KB;
-  const WaitCtx wc{a.status, &abort_flag, a.wait_limit}, wl{a.status, &abort_flag, a.wait_limit, true};
+  const WaitCtx wc{a.status, &abort_flag, a.wait_limit, true}, wl = wc;
 
   // ---- units before each request (both CTAs of a pair read the same lengths and come to the same list)
   pdl_wait();
@@ -308,7 +289,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   auto index_of = [&](int k) { return k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair); };
   auto unit_at = [&](int j) {
     Unit u;
-    u.index = j, u.range = a.ranges > 1 ? j % a.ranges : 0;
+    u.range = a.ranges > 1 ? j % a.ranges : 0, u.pad = 0;
     const int uh = a.ranges > 1 ? j / a.ranges : j, ut = a.hkv > 1 ? uh / a.hkv : uh;
     u.hk = uh - ut * a.hkv;
     int lo = 0, hi = a.pb.batch;                    // s_first[lo] <= ut < s_first[hi]
@@ -338,6 +319,15 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     u.r.b = -1, u.T = 0;
     return u;
   };
+  // The units come through shared memory from a warp of their own: some 400 instructions each (searches, divisions), which every warp
+  // would else run between its units (20 warps: 2000 clocks of the schedulers' time per unit).
+  auto unit = [&](int i) {                          // the i-th unit of this pair, by a whole warp, in turn
+    wait_warp(smem_u32(&u_full[i % UNITS]), (uint32_t)(i / UNITS) & 1u, wl);
+    const Unit u = s_unit[i % UNITS];
+    __syncwarp();
+    if (lane == 0) mbar_arrive_local(smem_u32(&u_free[i % UNITS]));
+    return u;
+  };
   // row of the planes of key `key` of a unit's request; past the pool where the request has no page for it (or a wrong entry)
   const int past = a.pb.n_pages << a.pb.page_shift;
   auto row_of = [&](const PagedRequest& r, int key) {
@@ -356,10 +346,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   if (warp == 0) {
     // =========================== K: a buffer is free again once the logits of the tile NB before exist ==================
     const int nc = np * (DH / 64 / cb), pc = lane % np, ch = (lane / np) * cb;        // copies of a block: one per lane
-    int k = 0, n = 0, i = 0;
+    int n = 0, i = 0;
     Ring<NB> rg;
-    Unit u = next_unit(k);
-    while (u.r.b >= 0) {
+    for (Unit u = unit(0); u.r.b >= 0; u = unit(++i)) {
       for (int t = 0; t < u.T; ++t, ++n, rg.next()) {
         const int row = lane < nc ? row_of(u.r, (u.t0 + t) * KB + half * 64 + (pc << piece_shift)) : 0;
         const int bf = rg.at;
@@ -376,21 +365,31 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
           __syncwarp();
           if (lane < DH / 64)
             copy4d(Qs + (uint32_t)lane * (128 * 128), &tmq, u.hk * G, u.r.lo + u.tok0 + half * TOK, lane, smem_u32(&q_full) & LEADER_MASK);
-          ++i;
         }
       }
-      u = next_unit(k);
     }
     __syncwarp();
+  } else if (warp == 2) {
+    // =========================== the pair's units ============================================================================
+    int k = 0;
+    for (int i = 0;; ++i) {
+      const Unit u = next_unit(k);
+      if (i >= UNITS) wait_warp(smem_u32(&u_free[i % UNITS]), (uint32_t)(i / UNITS - 1) & 1u, wl);
+      if (lane == 0) {
+        s_unit[i % UNITS] = u;
+        mbar_arrive_local(smem_u32(&u_full[i % UNITS]));
+      }
+      __syncwarp();
+      if (u.r.b < 0) break;
+    }
   } else if (warp == 1) {
     // =========================== V: a buffer is free again once P V of the tile NB before has completed ==================
     const uint32_t full_lead = map_rank(smem_u32(&v_full[0]), 0);
     const int nb = np * (DH / 128 / cb), blk = lane / nb, pc = lane % np, ch = ((lane % nb) / np) * cb;   // copies of a block; block of this lane
     uint32_t ph_own = 0;
-    int k = 0, n = 0;
+    int n = 0, i = 0;
     Ring<NB> rg;
-    Unit u = next_unit(k);
-    while (u.r.b >= 0) {
+    for (Unit u = unit(0); u.r.b >= 0; u = unit(++i)) {
       for (int t = 0; t < u.T; ++t, ++n, rg.next()) {
         const int key0 = (u.t0 + t) * KB, rem = u.r.kv - key0;                        // rows past the cached tokens: rem .. of the tile
         // (rows up to the end of the piece that they begin in; later pieces are zeros)
@@ -423,7 +422,6 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
           if (lane == 0) remote_arrive_stores(full_lead + (uint32_t)bf * 8u);
         }
       }
-      u = next_unit(k);
     }
     __syncwarp();
   } else if (warp == 3) {
@@ -434,46 +432,63 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     // the scheduler, 3400 per tile.  Two warps, one per product: 2770, as S(n + NB) then waits for the completion of P(n) V(n).)
     if (half == 0) {
       const uint32_t elected = elect_one() ? 1u : 0u;
-      int k = 0, ahead = 0, ts = 0, kp = 0;                       // ahead: logits issued whose P V has not been; ts: tile of the unit
-      uint32_t par_q = 0, par_o = 1;
+      // ahead: logits issued whose P V has not been; left: tiles of the unit whose logits are to come.  The logits' unit is this one or the next.
+      int ahead = 0, left = 0, i = 0;
+      uint32_t par_q = 1, par_o = 1;
       Ring<NB> rs, rp;
-      Unit us = next_unit(k);
-      const uint64_t dq = make_desc(Qs);
-      auto logits = [&] {
-        wait_warp(smem_u32(&k_full[rs.at]), rs.parity, wc);
-        if (ts == 0) wait_warp(smem_u32(&q_full), par_q, wc);
-        tc_fence_after();
-        const uint64_t db = make_desc(Ks + (uint32_t)rs.at * L::TILE);      // (a 64-channel block further: 128 x 128 and 64 x 128 bytes)
-#pragma unroll
-        for (int c = 0; c < DH / 64; ++c)
-          umma2_ss_x4(tmem_s + (uint32_t)rs.at * KB, dq + (uint64_t)(c * ((128 * 128) >> 4)), db + (uint64_t)(c * (L::KBLOCK >> 4)), IDESC_S, c == 0 ? 1u : 0u, elected);
-        if (elected) umma2_commit(smem_u32(&s_full[rs.at]));
-        rs.next(), ++ahead;
-        if (++ts == us.T) {
-          if (elected) umma2_commit(smem_u32(&q_free));
-          ts = 0, par_q ^= 1u, us = next_unit(k);
-        }
-      };
-      int i = 0;
-      for (Unit u = next_unit(kp); u.r.b >= 0; u = next_unit(kp), par_o ^= 1u, ++i) {
-        for (int t = 0; t < u.T; ++t, rp.next()) {
+      const uint32_t k_bar = smem_u32(&k_full[0]), s_bar = smem_u32(&s_full[0]), v_bar = smem_u32(&v_full[0]), p_bar = smem_u32(&p_full[0][0]), d_bar = smem_u32(&pv_done[0]);
+      const uint64_t dq = make_desc(Qs), dk = make_desc(Ks), dv = make_desc_mn(Vs, L::KBLOCK, 1024);
+      Unit u = unit(0), nx = u;
+      bool next_begun = true;                                     // (the logits' unit is nx)
+      if (u.r.b >= 0) {
+        left = u.T, par_q ^= 1u;
+        wait_warp(smem_u32(&q_full), par_q, wc);
+        nx = unit(1), next_begun = false;
+      }
+      for (; u.r.b >= 0; ++i, par_o ^= 1u) {
+        const int ends = u.r.kv < (u.t0 + u.T) * KB ? u.T - 1 : -1;       // the tile in which the cached tokens end: rows of it were cleared by a warp of each CTA
+        for (int t = 0; t < u.T; ++t) {
           // Logits as far ahead as there are buffers; those of the next unit only once its queries are there, or nothing else is left
-          while (us.r.b >= 0 && ahead < NB && (ts > 0 || ahead == 0 || __all_sync(0xffffffffu, mbar_test(smem_u32(&q_full), par_q)))) logits();
-          const uint32_t pf = smem_u32(&p_full[rp.at][0]), vb = Vs + (uint32_t)rp.at * L::TILE;
-          wait_warp(smem_u32(&v_full[rp.at]), rp.parity, wc);
-          // (the tile in which the cached tokens end: rows of it were cleared by a warp of each CTA)
-          if (u.r.kv < (u.t0 + t + 1) * KB) pair_acquire(smem_u32(&v_full[rp.at]), rp.parity);
+          do {
+            if (left == 0) {
+              if (next_begun || nx.r.b < 0 || !(ahead == 0 || __all_sync(0xffffffffu, mbar_test(smem_u32(&q_full), par_q ^ 1u)))) break;
+              left = nx.T, par_q ^= 1u, next_begun = true;
+              wait_warp(smem_u32(&q_full), par_q, wc);
+            }
+            wait_warp(k_bar + 8u * rs.at, rs.parity, wc);
+            tc_fence_after();
+            const uint64_t db = dk + (uint64_t)((uint32_t)rs.at * (L::TILE >> 4));      // (a 64-channel block further: 128 x 128 and 64 x 128 bytes)
+#pragma unroll
+            for (int c = 0; c < DH / 64; ++c)
+              umma2_ss_x4(tmem_s + (uint32_t)rs.at * KB, dq + (uint64_t)(c * ((128 * 128) >> 4)), db + (uint64_t)(c * (L::KBLOCK >> 4)), IDESC_S, c == 0 ? 1u : 0u, elected);
+            if (elected) {
+              umma2_commit(s_bar + 8u * rs.at);
+              if (left == 1) umma2_commit(smem_u32(&q_free));
+            }
+            rs.next(), ++ahead, --left;
+          } while (ahead < NB);
+          wait_warp(v_bar + 8u * rp.at, rp.parity, wc);
+          if (t == ends) pair_acquire(v_bar + 8u * rp.at, rp.parity);
           if (t == 0 && i > 0) wait_warp(smem_u32(&o_free), par_o, wc);
 #pragma unroll
           for (int kh = 0; kh < 2; ++kh) {
-            wait_warp(pf + 8u * kh, rp.parity, wc);
+            wait_warp(p_bar + 16u * rp.at + 8u * kh, rp.parity, wc);
             tc_fence_after();
             // A = P of this tile: bf16 pairs in the first 64 columns of its S buffer
-            umma2_ts_x4(tmem_o, tmem_s + (uint32_t)rp.at * KB + (uint32_t)kh * 32, make_desc_mn(vb + (uint32_t)kh * L::PIECE, L::KBLOCK, 1024), IDESC_PV,
+            umma2_ts_x4(tmem_o, tmem_s + (uint32_t)rp.at * KB + (uint32_t)kh * 32, dv + (uint64_t)((uint32_t)rp.at * (L::TILE >> 4) + kh * (L::PIECE >> 4)), IDESC_PV,
                         t == 0 && kh == 0 ? 1u : 0u, elected);
           }
-          if (elected) umma2_commit(smem_u32(&pv_done[rp.at]));
-          --ahead;
+          if (elected) umma2_commit(d_bar + 8u * rp.at);
+          rp.next(), --ahead;
+        }
+        // (with units of one tile the logits of the next one may be all issued: then on to the one behind it)
+        u = nx;
+        if (u.r.b >= 0) {
+          if (!next_begun) {
+            left = u.T, par_q ^= 1u;
+            wait_warp(smem_u32(&q_full), par_q, wc);
+          }
+          nx = unit(i + 2), next_begun = false;
         }
       }
     }
@@ -495,12 +510,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
       out_off[x] = (rt * a.hq + r - rt * G) * DH + c0 + (lane & 1) * 8;
     }
     bool odd = false;
-    int k = 0, n = 0, i = 0;
+    int n = 0, i = 0;
     Ring<NB> rg;
     uint32_t last_bar = 0, last_par = 0;      // of the tile before: its P V complete
-    Unit u = next_unit(k);
-    for (; u.r.b >= 0; ++i) {
-      const Unit me = u;
+    for (Unit me = unit(0); me.r.b >= 0; me = unit(++i)) {
       const int tok = me.tok0 + half * TOK + row_tok;
       const bool live = row < TOK * G && tok < me.r.n;
       // (rows of no token count as seeing all: masked, they would keep their warps in the masked form of every tile)
@@ -514,7 +527,6 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
         if (lane == 0) remote_arrive(pfull0 + (uint32_t)rg.at * 16u);
         last_bar = smem_u32(&pv_done[rg.at]), last_par = rg.parity;
       }
-      u = next_unit(k);                       // (the next one, while the last product runs)
       // ---- output: O / l -> bf16, 16 columns at a time through a staging block of the warp, out in whole sectors; or the accumulator
       // of a key range as it is.  A rolled loop: run once per unit, its code comes from far at about 11 clocks an instruction.
       xsum[i & 1][g][row] = l;
@@ -529,8 +541,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
       const size_t slot = ((size_t)me.range * a.pb.tokens + first_tok + row_tok) * a.hq + me.hk * G + (row - row_tok * G);
       if (g == 0 && a.ranges > 1 && row < n_rows) a.part_ml[slot] = make_float4(m, sum, (float)me.ranges, 0.f);
       __nv_bfloat16* ob = (__nv_bfloat16*)a.out + ((size_t)first_tok * a.hq + me.hk * G) * DH;
-      const uint64_t inv2 = pack2(inv, inv);
-      uint64_t fin2 = 0;
+      float fin = 0.f;
 #pragma unroll 1
       for (int c = 0; c < DH / 4; c += 16, ob += 16) {
         float o[16];
@@ -547,17 +558,14 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
             for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
 #pragma unroll
-          for (int e = 0; e < 16; e += 2) fin2 = fma2(pack2(o[e], o[e + 1]), 0ull, fin2);
+          for (int e = 0; e < 16; ++e) fin = fmaf(o[e], 0.f, fin);
           continue;
         }
         uint32_t w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const uint64_t o2 = pack2(o[2 * e], o[2 * e + 1]);
-          float e0, e1;
-          fin2 = fma2(o2, 0ull, fin2);        // (NaN of an infinity or a NaN)
-          unpack2(fma2(o2, inv2, 0ull), e0, e1);
-          w[e] = pack_bf16(e0, e1);
+          fin = fmaf(o[2 * e], 0.f, fin), fin = fmaf(o[2 * e + 1], 0.f, fin);        // (NaN of an infinity or a NaN)
+          w[e] = pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e)
@@ -575,9 +583,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
         }
         __syncwarp();
       }
-      float f0, f1;
-      unpack2(fin2, f0, f1);
-      odd |= row < n_rows && !(f0 + f1 == 0.f);
+      odd |= row < n_rows && !(fin == 0.f);
     }
     // ---- rows that are not finite although the values that they see may be: those of them with an infinity or a NaN among the keys of
     // their tiles that they do not see once more, key by key (channel by channel right otherwise: an infinite value is of one channel)
@@ -586,8 +592,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
       rows_sync(q);                           // (maxima beside a range's result: written by another warp of the quarter)
     }
     if (a.causal && __any_sync(0xffffffffu, odd) && !*reinterpret_cast<volatile int*>(&abort_flag)) {
-      k = 0;
-      for (u = next_unit(k); u.r.b >= 0; u = next_unit(k)) {
+      int k = 0;
+      for (Unit u = next_unit(k); u.r.b >= 0; u = next_unit(k)) {
         const int n_rows = min(TOK, u.r.n - u.tok0 - half * TOK) * G, end = min((u.t0 + u.T) * KB, u.r.kv);
         for (int rr = q * 32; rr < min(n_rows, q * 32 + 32); ++rr) {
           constexpr int C = DH / 128;         // channels of a lane, of this warp's
