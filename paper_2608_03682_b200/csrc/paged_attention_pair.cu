@@ -30,8 +30,7 @@ namespace {
 
 constexpr int KB = 128;                        // keys per tile: two blocks of 64
 constexpr int PP_THREADS = 20 * 32;
-constexpr int PAIR_LEAST = 2;                  // tiles of keys in a range, at least
-constexpr int PAIR_PIECES = 3;                 // ranges a pair takes where units are split
+constexpr int PAIR_LEAST = 2;                  // tiles of keys in a range where units are split, at least
 
 template <int DH>
 struct PpLayout {
@@ -241,18 +240,37 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   pdl_wait();
   if (tid == 0) s_skip = status_set(a.status), s_first[0] = 0;
   bool bad = false;
-  int acc = 0;
-  long long tiles_all = 0;                          // of whole requests' units: at least what the units have
+  int longest = 0x7fffffff;                         // tiles of a key range
+  if (a.ranges > 1) {
+    // such that there are about two ranges for each pair, and not many more (a unit's last range is half as long on average)
+    long long tiles = 0;
+    int units = 0;
+    for (int i = tid; i < a.pb.batch; i += PP_THREADS) {
+      const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1], kv = a.pb.kv_lens[i];
+      if (paged_entry_bad(a.pb, i, lo, hi, kv, false)) continue;
+      const int n = (hi - lo + 2 * TOK - 1) / (2 * TOK);
+      units += n, tiles += (long long)n * ((kv + KB - 1) / KB);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, o), units += __shfl_xor_sync(0xffffffffu, units, o);
+    if (lane == 0) s_sum[warp] = tiles, s_warp[warp] = units;
+    __syncthreads();
+    tiles = 0, units = 0;
+    for (int w = 0; w < PP_THREADS / 32; ++w) tiles += s_sum[w], units += s_warp[w];
+    __syncthreads();
+    const long long pieces = 2ll * n_pairs - (long long)units * a.hkv / 2, per = pieces > 0 ? (tiles * a.hkv + pieces - 1) / pieces : 0x7fffffff;
+    longest = (int)(per < PAIR_LEAST ? PAIR_LEAST : per > 0x7fffffff ? 0x7fffffff : per);
+  }
+  auto ranges_for = [&](int kv) { return a.ranges > 1 ? min(a.ranges, max(1, ((kv + KB - 1) / KB - 1) / longest + 1)) : 1; };
+  int acc = 0;                                      // key ranges of units (of one kv head) so far
   for (int i0 = 0; i0 < a.pb.batch; i0 += PP_THREADS) {
     const int i = i0 + tid;
     int n = 0;
     if (i < a.pb.batch) {
-      const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1];
-      const int kv = a.pb.kv_lens[i];
+      const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1], kv = a.pb.kv_lens[i];
       const bool b = paged_entry_bad(a.pb, i, lo, hi, kv, false);
       bad |= b;
-      n = b ? 0 : (hi - lo + 2 * TOK - 1) / (2 * TOK);
-      tiles_all += (long long)n * ((kv + KB - 1) / KB);
+      n = b ? 0 : (hi - lo + 2 * TOK - 1) / (2 * TOK) * ranges_for(kv);
     }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -272,26 +290,14 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   bad = __syncthreads_or(bad);
   if (bad && tid == 0) atomicExch(a.status, ST_INVALID_ARG);
   const bool skip = s_skip != 0;
-  const int n_units = bad ? 0 : acc * a.hkv * a.ranges;
-  int least = PAIR_LEAST;
-  if (a.ranges > 1) {                               // tiles of a range: three ranges a pair
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) tiles_all += __shfl_xor_sync(0xffffffffu, tiles_all, o);
-    if (lane == 0) s_sum[warp] = tiles_all;
-    __syncthreads();
-    tiles_all = 0;
-    for (int w = 0; w < PP_THREADS / 32; ++w) tiles_all += s_sum[w];
-    const long long per = tiles_all * a.hkv / (PAIR_PIECES * n_pairs);
-    least = (int)(per < PAIR_LEAST ? PAIR_LEAST : per > 0x7fffffff ? 0x7fffffff : per);
-  }
+  const int n_units = bad ? 0 : acc * a.hkv;
 
   // Units of this pair: of every round of n_pairs units one, rounds dealt back and forth (a request's last, longest tiles come first).
   auto index_of = [&](int k) { return k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair); };
   auto unit_at = [&](int j) {
     Unit u;
-    u.range = a.ranges > 1 ? j % a.ranges : 0, u.pad = 0;
-    const int uh = a.ranges > 1 ? j / a.ranges : j, ut = a.hkv > 1 ? uh / a.hkv : uh;
-    u.hk = uh - ut * a.hkv;
+    const int ut = a.hkv > 1 ? j / a.hkv : j;
+    u.hk = j - ut * a.hkv, u.pad = 0;
     int lo = 0, hi = a.pb.batch;                    // s_first[lo] <= ut < s_first[hi]
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -300,9 +306,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     }
     u.r.b = lo, u.r.lo = a.pb.cu[lo], u.r.n = a.pb.cu[lo + 1] - u.r.lo, u.r.kv = a.pb.kv_lens[lo];
     u.r.prefix = a.prefix_lens ? min(max(a.prefix_lens[lo], 0), u.r.kv) : 0;
-    u.tok0 = (s_first[lo + 1] - 1 - ut) * 2 * TOK;
+    const int ranges = ranges_for(u.r.kv), from_end = s_first[lo + 1] - 1 - ut, ui = from_end / ranges;
+    u.tok0 = ui * 2 * TOK, u.range = from_end - ui * ranges;
     const int keys = u.r.limit(min(u.tok0 + 2 * TOK, u.r.n) - 1, a.causal), tiles = max(1, (keys + KB - 1) / KB);
-    u.ranges = ranges_of(tiles, a.ranges, least);
+    u.ranges = min(ranges, tiles);                  // (none of them empty)
     u.t0 = u.range < u.ranges ? (int)((long long)tiles * u.range / u.ranges) : 0;
     u.T = u.range < u.ranges ? (int)((long long)tiles * (u.range + 1) / u.ranges) - u.t0 : 0;
     return u;
