@@ -473,38 +473,61 @@ __global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
 // =============================================================================================
 // merge of key ranges
 // =============================================================================================
-// A warp per row: weights 2^(m_r - max m), fixed order of the ranges.
+// A warp per row: weights 2^(m_r - max m), in the order of the ranges; a lane takes DH / 32 channels, four ranges' loads at a time.
 template <int DH, typename OUT>
 __global__ void __launch_bounds__(128) k_paged_merge(const PagedAttn a) {
-  constexpr int C = DH / 32;
+  constexpr int C = DH / 32, V = C < 4 ? C : 4;             // channels of a lane, of a load
   const int lane = threadIdx.x & 31, c = lane * C;
   const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5), rows = (long long)a.pb.tokens * a.hq;
   pdl_launch_dependents();
   pdl_wait();
-  if (status_set(a.status) || row >= rows) return;
+  if (row >= rows) return;
   const int tok = (int)(row / a.hq);
-  if (tok < a.pb.cu[0] || tok >= a.pb.cu[a.pb.batch]) return;
-  const int ranges = (int)a.part_ml[row].z;
+  // (the lengths and the word say whether there is anything in the workspace; its entries are on their way meanwhile)
+  const bool live = !status_set(a.status) && tok >= a.pb.cu[0] && tok < a.pb.cu[a.pb.batch];
+  const int most = a.ranges;
+  float4 ml = lane < most ? a.part_ml[(size_t)lane * rows + row] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  if (!live) return;
+  const int ranges = (int)__shfl_sync(0xffffffffu, ml.z, 0);
   if (ranges <= 1) return;
-  float M = -INFINITY;
-  for (int k = lane; k < ranges; k += 32) M = fmaxf(M, a.part_ml[(size_t)k * rows + row].x);
-  M = warp_max(M);
-  float o[C] = {}, sum = 0.f;
-#pragma unroll 4
-  for (int k = 0; k < ranges; ++k) {
-    const float4 ml = a.part_ml[(size_t)k * rows + row];
-    const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-    sum = fmaf(w, ml.y, sum);
-    const float* p = a.part_o + ((size_t)k * rows + row) * DH + c;
+  float4 ml2 = make_float4(-INFINITY, 0.f, 0.f, 0.f);       // (up to 64 ranges)
+  if (lane + 32 < ranges) ml2 = a.part_ml[(size_t)(lane + 32) * rows + row];
+  if (lane >= ranges) ml = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  const float M = warp_max(fmaxf(ml.x, ml2.x));
+  const float w1 = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M), w2 = ml2.x == -INFINITY ? 0.f : exp2f(ml2.x - M);
+  const float sum = warp_sum(w1 * ml.y + w2 * ml2.y);
+  float o[C] = {};
+  const float* p = a.part_o + (size_t)row * DH + c;
+  for (int k0 = 0; k0 < ranges; k0 += 4) {
+    float x[4][C];
 #pragma unroll
-    for (int e = 0; e < C; ++e) o[e] = fmaf(w, p[e], o[e]);
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < C; e += V) {
+        if (k0 + j >= ranges) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) x[j][e + v] = 0.f;
+        } else if constexpr (V == 4) {
+          const float4 v = *reinterpret_cast<const float4*>(p + (size_t)(k0 + j) * rows * DH + e);
+          x[j][e] = v.x, x[j][e + 1] = v.y, x[j][e + 2] = v.z, x[j][e + 3] = v.w;
+        } else {
+          const float2 v = *reinterpret_cast<const float2*>(p + (size_t)(k0 + j) * rows * DH + e);
+          x[j][e] = v.x, x[j][e + 1] = v.y;
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float w = __shfl_sync(0xffffffffu, k0 + j < 32 ? w1 : w2, (k0 + j) & 31);      // (0 past the ranges)
+#pragma unroll
+      for (int e = 0; e < C; ++e) o[e] = fmaf(w, x[j][e], o[e]);
+    }
   }
   const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
   OUT* dst = (OUT*)a.out + row * DH + c;
 #pragma unroll
-  for (int e = 0; e < C; ++e) {
-    if constexpr (sizeof(OUT) == 4) dst[e] = o[e] * inv;
-    else dst[e] = __float2bfloat16_rn(o[e] * inv);
+  for (int e = 0; e < C; e += 2) {
+    if constexpr (sizeof(OUT) == 4) *reinterpret_cast<float2*>(dst + e) = make_float2(o[e] * inv, o[e + 1] * inv);
+    else *reinterpret_cast<uint32_t*>(dst + e) = pack_bf16(o[e] * inv, o[e + 1] * inv);
   }
 }
 
