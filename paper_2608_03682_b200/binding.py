@@ -543,31 +543,44 @@ def _launch(device: torch.device, stream):
     return _HERE_ON[i] if stream is None and i < 64 and i == torch._C._cuda_getDevice() else _Elsewhere(device, stream)
 
 
-def _head_rows(name: str, t: torch.Tensor, device: torch.device, dtype: Optional[torch.dtype] = None) -> int:
-    """Checks rows of heads ``[T, heads, dh]`` (heads contiguous in a row); returns the row stride in elements."""
-    if t.dim() != 3 or t.dtype not in _STORE or t.device != device or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{name} must be a {dtype or 'float32 or bfloat16'} tensor [tokens, heads, head_dim] on {device}")
+_I32, _F32 = torch.int32, torch.float32
+
+
+def _head_rows(name: str, t: torch.Tensor, device: torch.device, dtype: torch.dtype) -> tuple:
+    """Checks rows of heads ``[T, heads, dh]`` (heads contiguous in a row); returns (T, heads, dh, row stride in elements)."""
+    if t.dtype is not dtype or t.device != device or t.dim() != 3:
+        raise ValueError(f"{name} must be a {dtype} tensor [tokens, heads, head_dim] on {device}")
     T, H, dh = t.shape
     row, head, one = t.stride()
     if one != 1 or (head != dh and H > 1):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
-    return row if T > 1 else H * dh
+    return T, H, dh, row if T > 1 else H * dh
 
 
 def _ints(name: str, t: torch.Tensor, device: torch.device, shape: tuple) -> int:
-    if t.dtype is not torch.int32 or t.shape != shape or t.device != device or not t.is_contiguous():
+    if t.dtype is not _I32 or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
     return t.data_ptr()
 
 
-def _floats(name: str, t: torch.Tensor, device: torch.device, shape: tuple) -> int:
-    if t.dtype is not torch.float32 or t.shape != shape or t.device != device or not t.is_contiguous():
+def _floats(name: str, t: Optional[torch.Tensor], device: torch.device, shape: tuple) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not _F32 or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous float32 tensor {list(shape)} on {device}")
     return t.data_ptr()
 
 
-def _rope(t: torch.Tensor, device: torch.device, dh: int) -> int:
-    return _floats("rope_cos_sin", t, device, (t.shape[0], dh // 2, 2))
+def _rope(t: Optional[torch.Tensor], device: torch.device, dh: int) -> tuple:
+    """(address, positions) of a table of cosines and sines."""
+    if t is None:
+        return None, 0
+    n = t.shape[0]
+    return _floats("rope_cos_sin", t, device, (n, dh // 2, 2)), n
+
+
+def _empty_rows(T: int, H: int, dh: int, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+    return torch.empty_strided((T, H, dh), (H * dh, dh, 1), dtype=dtype, device=device)
 
 
 _heads_descs: Dict[tuple, tuple] = {}     # sizes and types of a call's heads -> (descriptor, its address)
@@ -594,31 +607,33 @@ def norm_rope_heads(q: Optional[torch.Tensor], k: torch.Tensor, positions: Optio
     ``positions`` (int32 ``[T]``) in the same pass; rows may be columns of a fused matrix.  Returns (q, k) in ``dtype`` (default: as
     given).  ``status``: int32 word that a position outside the table raises (zeroed by the caller; None: a fresh one, not returned)."""
     lib = _lib or load_library()
-    device = k.device
-    k_row = _head_rows("k", k, device)
-    T, Hkv, dh = k.shape
-    Hq = q_row = 0
+    device, src = k.device, k.dtype
+    if src not in _STORE:
+        raise ValueError("k must be a float32 or bfloat16 tensor [tokens, heads, head_dim]")
+    T, Hkv, dh, k_row = _head_rows("k", k, device, src)
+    Hq, q_row, q_ptr, q_out, q_out_ptr = 0, 0, None, None, None
     if q is not None:
-        q_row = _head_rows("q", q, device, k.dtype)
-        Tq, Hq, dq = q.shape
+        Tq, Hq, dq, q_row = _head_rows("q", q, device, src)
         if Tq != T or dq != dh:
             raise ValueError("q and k differ in tokens or head_dim")
-    dtype = dtype or k.dtype
-    if dtype not in _STORE:
+        q_ptr = q.data_ptr()
+    if dtype is None:
+        dtype = src
+    elif dtype not in _STORE:
         raise ValueError("dtype must be float32 or bfloat16")
-    desc = _heads_desc(Hq, Hkv, dh, _STORE[k.dtype], _STORE[dtype], eps)
-    rope = None if rope_cos_sin is None else _rope(rope_cos_sin, device, dh)
-    gq = None if q_gain is None else _floats("q_gain", q_gain, device, (dh,))
-    gk = None if k_gain is None else _floats("k_gain", k_gain, device, (dh,))
+    desc = _heads_desc(Hq, Hkv, dh, _STORE[src], _STORE[dtype], eps)
+    rope, n_pos = _rope(rope_cos_sin, device, dh)
+    gq, gk = _floats("q_gain", q_gain, device, (dh,)), _floats("k_gain", k_gain, device, (dh,))
     pos = None if positions is None else _ints("positions", positions, device, (T,))
     with _launch(device, stream) as sp:
-        q_out = None if q is None else torch.empty((T, Hq, dh), dtype=dtype, device=device)
-        k_out = torch.empty((T, Hkv, dh), dtype=dtype, device=device)
+        if q is not None:
+            q_out = _empty_rows(T, Hq, dh, dtype, device)
+            q_out_ptr = q_out.data_ptr()
+        k_out = _empty_rows(T, Hkv, dh, dtype, device)
         if status is None:
             status = torch.zeros(1, dtype=torch.int32, device=device)
-        st = lib.phyai_norm_rope_heads(desc[1], T, None if q is None else q.data_ptr(), q_row, k.data_ptr(), k_row, pos, rope,
-                                       0 if rope is None else rope_cos_sin.shape[0], gq, gk, None if q is None else q_out.data_ptr(),
-                                       k_out.data_ptr(), _ints("status", status, device, (1,)), sp)
+        st = lib.phyai_norm_rope_heads(desc[1], T, q_ptr, q_row, k.data_ptr(), k_row, pos, rope, n_pos, gq, gk, q_out_ptr, k_out.data_ptr(),
+                                       _ints("status", status, device, (1,)), sp)
     if st != OK:
         _paged_fail(lib, st)
     return q_out, k_out
@@ -654,40 +669,42 @@ class PagedCache:
         return st
 
     def _requests(self, cu_q_lens, kv_lens, page_table):
-        if page_table.dim() != 2:
+        device, shape = self.device, page_table.shape
+        if len(shape) != 2:
             raise ValueError("page_table must be [batch, max_pages]")
-        device = self.device
-        B, most = shape = page_table.shape
-        cu = None if cu_q_lens is None else _ints("cu_q_lens", cu_q_lens, device, (B + 1,))
-        return B, most, cu, _ints("kv_lens", kv_lens, device, (B,)), _ints("page_table", page_table, device, shape)
+        B, most = shape
+        return (B, most, None if cu_q_lens is None else _ints("cu_q_lens", cu_q_lens, device, (B + 1,)), _ints("kv_lens", kv_lens, device, (B,)),
+                _ints("page_table", page_table, device, shape))
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, cu_q_lens: torch.Tensor, kv_lens: torch.Tensor, page_table: torch.Tensor,
                rope_cos_sin: Optional[torch.Tensor], k_gain: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
                q_gain: Optional[torch.Tensor] = None, eps: float = 1e-6, positions: Optional[torch.Tensor] = None, stream=None):
         """New keys (normed with gain ``1 + k_gain`` unless None, rotated) and values ``[T, Hkv, dh]`` into the pages of ``layer``; with
         ``q`` ``[T, Hq, dh]`` returns its normed, rotated rows in the cache's type (rows of no request are not written), else None."""
-        lib, device = self.lib, self.device
-        k_row, v_row = _head_rows("k", k, device), _head_rows("v", v, device, k.dtype)
-        T, Hkv, dh = k.shape
-        if v.shape != k.shape:
+        lib, device, src = self.lib, self.device, k.dtype
+        if src not in _STORE:
+            raise ValueError("k must be a float32 or bfloat16 tensor [tokens, heads, head_dim]")
+        T, Hkv, dh, k_row = _head_rows("k", k, device, src)
+        Tv, Hv, dv, v_row = _head_rows("v", v, device, src)
+        if Tv != T or Hv != Hkv or dv != dh:
             raise ValueError("k and v differ in tokens, heads or head_dim")
-        Hq = q_row = 0
+        Hq, q_row, q_ptr, q_out, q_out_ptr = 0, 0, None, None, None
         if q is not None:
-            q_row = _head_rows("q", q, device, k.dtype)
-            Tq, Hq, dq = q.shape
+            Tq, Hq, dq, q_row = _head_rows("q", q, device, src)
             if Tq != T or dq != dh:
                 raise ValueError("q and k differ in tokens or head_dim")
-        desc = _heads_desc(Hq, Hkv, dh, _STORE[k.dtype], self._desc.dtype, eps)
+            q_ptr = q.data_ptr()
+        desc = _heads_desc(Hq, Hkv, dh, _STORE[src], self._desc.dtype, eps)
         B, most, cu, lens, table = self._requests(cu_q_lens, kv_lens, page_table)
-        rope = None if rope_cos_sin is None else _rope(rope_cos_sin, device, dh)
-        gq = None if q_gain is None else _floats("q_gain", q_gain, device, (dh,))
-        gk = None if k_gain is None else _floats("k_gain", k_gain, device, (dh,))
+        rope, n_pos = _rope(rope_cos_sin, device, dh)
+        gq, gk = _floats("q_gain", q_gain, device, (dh,)), _floats("k_gain", k_gain, device, (dh,))
         pos = None if positions is None else _ints("positions", positions, device, (T,))
         with _launch(device, stream) as sp:
-            q_out = None if q is None else torch.empty((T, Hq, dh), dtype=self.dtype, device=device)
-            st = lib.phyai_append_paged_kv(self._desc_ptr, desc[1], layer, T, None if q is None else q.data_ptr(), q_row, k.data_ptr(), k_row,
-                                           v.data_ptr(), v_row, B, cu, lens, table, most, pos, rope, 0 if rope is None else rope_cos_sin.shape[0],
-                                           gq, gk, None if q is None else q_out.data_ptr(), self._status_ptr, sp)
+            if q is not None:
+                q_out = _empty_rows(T, Hq, dh, self.dtype, device)
+                q_out_ptr = q_out.data_ptr()
+            st = lib.phyai_append_paged_kv(self._desc_ptr, desc[1], layer, T, q_ptr, q_row, k.data_ptr(), k_row, v.data_ptr(), v_row, B, cu, lens, table,
+                                           most, pos, rope, n_pos, gq, gk, q_out_ptr, self._status_ptr, sp)
         if st != OK:
             _paged_fail(lib, st)
         return q_out
@@ -698,13 +715,12 @@ class PagedCache:
         included.  ``causal``: a token sees what is cached before it and itself, and with ``prefix_lens`` (int32 ``[B]``) the first so many
         tokens.  Returns ``out`` ``[T, Hq, dh]`` (rows of no request are not written)."""
         lib, device = self.lib, self.device
-        row = _head_rows("q", q, device, self.dtype)
-        T, Hq, dh = shape = q.shape
+        T, Hq, dh, row = _head_rows("q", q, device, self.dtype)
         if dh != self.head_dim:
             raise ValueError("q and the cache differ in head_dim")
         B, most, cu, lens, table = self._requests(cu_q_lens, kv_lens, page_table)
         prefix = None if prefix_lens is None else _ints("prefix_lens", prefix_lens, device, (B,))
-        if out is not None and (out.shape != shape or out.dtype != q.dtype or out.device != device or not out.is_contiguous()):
+        if out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != device or not out.is_contiguous()):
             raise ValueError("out must be a contiguous tensor of q's shape and type")
         if scale is not None and not scale > 0.0:
             raise ValueError("scale must be positive")
@@ -716,7 +732,7 @@ class PagedCache:
                 need = self._work[Hq, T, B, most] = lib.phyai_paged_attention_workspace_bytes(self._desc_ptr, Hq, T, B, most)
             work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
             if out is None:
-                out = torch.empty(shape, dtype=self.dtype, device=device)
+                out = _empty_rows(T, Hq, dh, self.dtype, device)
             st = lib.phyai_paged_attention(self._desc_ptr, layer, Hq, T, q.data_ptr(), row, B, cu, lens, table, most, 1 if causal else 0, prefix,
                                            0.0 if scale is None else scale, out.data_ptr(), work.data_ptr() if need else None, need,
                                            self._status_ptr, sp)
