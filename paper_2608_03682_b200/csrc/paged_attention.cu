@@ -566,8 +566,7 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
     // tiles of 64 rows where there are enough of them for the SMs (17 tokens of 4 heads of 4 requests: 16-row tiles)
     p.rt = rows / 64 * c->n_kv_heads >= n_sm ? 64 : 16;
   } else {
-    const int most = c->head_dim == 64 ? 32 : 16;
-    p.rt = rows <= 8ll * holders ? 8 : rows <= 16ll * holders || most == 16 ? 16 : most;
+    p.rt = rows <= 8ll * holders ? 8 : 16;
   }
   p.units = rows / p.rt + holders;
   // parts of a row tile's keys: enough blocks for two on each SM, of at least 128 keys; up to eight of them are a cluster
@@ -690,7 +689,7 @@ phyai_status_t phyai_paged_attention(const phyai_paged_cache_t* cache, uint32_t 
       snprintf(g_paged_err, sizeof(g_paged_err), "cuTensorMapEncodeTiled failed");
       return PHYAI_ERR_CUDA;
     }
-    if (dh == 64) e = p.rt == 8 ? launch_few<64, 1>(a, p, map, st) : p.rt == 16 ? launch_few<64, 2>(a, p, map, st) : launch_few<64, 4>(a, p, map, st);
+    if (dh == 64) e = p.rt == 8 ? launch_few<64, 1>(a, p, map, st) : launch_few<64, 2>(a, p, map, st);
     else if (dh == 128) e = p.rt == 8 ? launch_few<128, 1>(a, p, map, st) : launch_few<128, 2>(a, p, map, st);
     else e = p.rt == 8 ? launch_few<256, 1>(a, p, map, st) : launch_few<256, 2>(a, p, map, st);
   }

@@ -30,17 +30,22 @@ namespace {
 
 constexpr int KB = 128;                        // keys per tile: two blocks of 64
 constexpr int PP_THREADS = 20 * 32;
+constexpr int PAIR_MERGE = 7;                  // tiles' time that splitting units costs
 constexpr int PAIR_LEAST = 2;                  // tiles of keys in a range where units are split, at least
 
+// head_dim 64: V counts as 128 channels, of which the second CTA's half is zero and never fetched (half of 64 channels would be 64 bytes a
+// key, another operand layout; the products are not what bounds that head_dim).
 template <int DH>
 struct PpLayout {
+  static constexpr int VN = DH < 128 ? 128 : DH;             // columns of the accumulator
   static constexpr int KBLOCK = 64 * 128;                    // 64 channels of 64 keys
-  static constexpr int PIECE = (DH / 128) * KBLOCK;          // 64 keys x DH / 2 channels
-  static constexpr int TILE = 2 * PIECE;                     // K: this CTA's block; V: both blocks, its channel half
+  static constexpr int PIECE = (VN / 128) * KBLOCK;          // V: 64 keys, this CTA's half of the channels
+  static constexpr int KTILE = (DH / 64) * KBLOCK;           // K: this CTA's block of 64 keys
+  static constexpr int VTILE = 2 * PIECE;                    // V: both blocks
   static constexpr int QTILE = 128 * DH * 2;
   static constexpr int STG = 1024;                           // output staging of a warp: 32 rows x 16 columns
-  static constexpr int NB = (512 - DH) / 128;                // buffers of logits: what the accumulator leaves of the 512 columns
-  static constexpr size_t SMEM = 1024 + 2 * NB * (size_t)TILE + QTILE + 16 * STG;
+  static constexpr int NB = (512 - VN) / 128;                // buffers of logits: what the accumulator leaves of the 512 columns
+  static constexpr size_t SMEM = 1024 + NB * (size_t)(KTILE + VTILE) + QTILE + 16 * STG;
 };
 
 __device__ __forceinline__ void copy4d(uint32_t dst, const CUtensorMap* map, int c1, int c2, int c3, uint32_t bar) {
@@ -194,7 +199,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   using L = PpLayout<DH>;
   constexpr int NB = L::NB;
   constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(KB >> 3) << 17) | ((256u >> 4) << 24);
-  constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((256u >> 4) << 24);
+  constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(L::VN >> 3) << 17) | ((256u >> 4) << 24);
 
   extern __shared__ uint8_t smem_raw[];
   // leader: operands of a buffer complete in both CTAs, P of a buffer (by column half) complete in both, Q complete in both, accumulator
@@ -206,6 +211,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   __shared__ float xch[2][4][128], xsum[2][4][128];       // what the four threads of a row exchange: maxima (by tile parity), sums (by unit parity)
   __shared__ int s_first[PAGED_MAX_BATCH + 1], s_warp[PP_THREADS / 32];
   __shared__ long long s_sum[PP_THREADS / 32];
+  __shared__ int s_most[PP_THREADS / 32];
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int half = blockIdx.x & 1, pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
@@ -213,7 +219,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   if (tid == 32) prefetch_tmap(&tmkv), prefetch_tmap(&tmq);
 
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t Ks = base, Vs = base + NB * L::TILE, Qs = base + 2 * NB * L::TILE;
+  const uint32_t Ks = base, Vs = base + NB * L::KTILE, Qs = Vs + NB * L::VTILE;
   if (tid == 0) {
     abort_flag = 0;
     for (int i = 0; i < NB; ++i) {
@@ -227,6 +233,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   if (warp == 3) {
     tmem_alloc2(smem_u32(&tmem_slot), 512);
     tc_fence_before();
+  }
+  if (DH < 128 && half == 1) {
+    for (uint32_t i = tid; i < NB * L::VTILE / 16; i += PP_THREADS) asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(Vs + i * 16), "r"(0u) : "memory");
+    fence_async_smem();
   }
   __syncthreads();
   pair_sync();                                      // both CTAs' barriers exist before the peer can signal them
@@ -244,22 +254,27 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   if (a.ranges > 1) {
     // such that there are about two ranges for each pair, and not many more (a unit's last range is half as long on average)
     long long tiles = 0;
-    int units = 0;
+    int units = 0, most = 0;
     for (int i = tid; i < a.pb.batch; i += PP_THREADS) {
       const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1], kv = a.pb.kv_lens[i];
       if (paged_entry_bad(a.pb, i, lo, hi, kv, false)) continue;
       const int n = (hi - lo + 2 * TOK - 1) / (2 * TOK);
       units += n, tiles += (long long)n * ((kv + KB - 1) / KB);
+      if (n) most = max(most, (kv + KB - 1) / KB);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, o), units += __shfl_xor_sync(0xffffffffu, units, o);
-    if (lane == 0) s_sum[warp] = tiles, s_warp[warp] = units;
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) s_sum[warp] = tiles, s_warp[warp] = units, s_most[warp] = most;
     __syncthreads();
     tiles = 0, units = 0;
-    for (int w = 0; w < PP_THREADS / 32; ++w) tiles += s_sum[w], units += s_warp[w];
+    for (int w = 0; w < PP_THREADS / 32; ++w) tiles += s_sum[w], units += s_warp[w], most = max(most, s_most[w]);
     __syncthreads();
     const long long pieces = 2ll * n_pairs - (long long)units * a.hkv / 2, per = pieces > 0 ? (tiles * a.hkv + pieces - 1) / pieces : 0x7fffffff;
     longest = (int)(per < PAIR_LEAST ? PAIR_LEAST : per > 0x7fffffff ? 0x7fffffff : per);
+    // (fp32 results and the second kernel cost what PAIR_MERGE tiles do: not where the longest units, left whole, end before that)
+    const long long whole = (long long)most * (((long long)units * a.hkv + n_pairs - 1) / n_pairs);
+    if (whole <= tiles * a.hkv / n_pairs + PAIR_MERGE) longest = 0x7fffffff;
   }
   auto ranges_for = [&](int kv) { return a.ranges > 1 ? min(a.ranges, max(1, ((kv + KB - 1) / KB - 1) / longest + 1)) : 1; };
   int acc = 0;                                      // key ranges of units (of one kv head) so far
@@ -347,7 +362,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     return (page << a.pb.page_shift) + (key & ((1 << a.pb.page_shift) - 1));
   };
   const int np = 64 >> piece_shift;                 // pieces of a block of 64 keys
-  const int cb = np == 1 ? DH / 128 : 1;            // blocks of 64 channels of a copy
+  const int cb = np == 1 ? L::VN / 128 : 1;         // blocks of 64 channels of a copy
   const uint32_t piece_bytes = (uint32_t)(128 << piece_shift);
 
   if (warp == 0) {
@@ -360,8 +375,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
         const int row = lane < nc ? row_of(u.r, (u.t0 + t) * KB + half * 64 + (pc << piece_shift)) : 0;
         const int bf = rg.at;
         if (n >= NB) wait_warp(smem_u32(&s_full[bf]), rg.parity ^ 1u, wl);
-        const uint32_t bar = smem_u32(&k_full[bf]), dst = Ks + (uint32_t)bf * L::TILE;
-        if (half == 0 && lane == 0) mbar_expect_tx(bar, (uint32_t)L::TILE * 2);
+        const uint32_t bar = smem_u32(&k_full[bf]), dst = Ks + (uint32_t)bf * L::KTILE;
+        if (half == 0 && lane == 0) mbar_expect_tx(bar, (uint32_t)L::KTILE * 2);
         __syncwarp();
         if (lane < nc) copy4d(dst + (uint32_t)ch * L::KBLOCK + (uint32_t)pc * piece_bytes, &tmkv, row, u.hk * (DH / 64) + ch, a.plane, bar & LEADER_MASK);
         if (t == 0) {                             // Q: its tile is free again once the last logits of the unit before exist
@@ -392,7 +407,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   } else if (warp == 1) {
     // =========================== V: a buffer is free again once P V of the tile NB before has completed ==================
     const uint32_t full_lead = map_rank(smem_u32(&v_full[0]), 0);
-    const int nb = np * (DH / 128 / cb), blk = lane / nb, pc = lane % np, ch = ((lane % nb) / np) * cb;   // copies of a block; block of this lane
+    const int nb = np * (L::VN / 128 / cb), blk = lane / nb, pc = lane % np, ch = ((lane % nb) / np) * cb;   // copies of a block; block of this lane
     uint32_t ph_own = 0;
     int n = 0, i = 0;
     Ring<NB> rg;
@@ -401,27 +416,27 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
         const int key0 = (u.t0 + t) * KB, rem = u.r.kv - key0;                        // rows past the cached tokens: rem .. of the tile
         // (rows up to the end of the piece that they begin in; later pieces are zeros)
         const int clear_to = (rem + (1 << piece_shift) - 1) >> piece_shift << piece_shift;
-        const bool clear = rem > 0 && rem < KB && clear_to > rem;
-        const int row = lane < 2 * nb ? row_of(u.r, key0 + blk * 64 + (pc << piece_shift)) : 0;
+        const bool fetch = DH >= 128 || half == 0, clear = fetch && rem > 0 && rem < KB && clear_to > rem;
+        const int row = fetch && lane < 2 * nb ? row_of(u.r, key0 + blk * 64 + (pc << piece_shift)) : 0;
         const int bf = rg.at;
-        const uint32_t dst = Vs + (uint32_t)bf * L::TILE;
+        const uint32_t dst = Vs + (uint32_t)bf * L::VTILE;
         uint32_t bar = smem_u32(&v_full[bf]);
         if (lane == 0) {
           if (n >= NB) wait(smem_u32(&pv_done[bf]), rg.parity ^ 1u, wl);
-          if (clear) mbar_expect_tx(smem_u32(&v_own), (uint32_t)L::TILE);
-          else if (half == 0) mbar_expect_tx(bar, 2 * (uint32_t)L::TILE);
+          if (clear) mbar_expect_tx(smem_u32(&v_own), (uint32_t)L::VTILE);
+          else if (half == 0) mbar_expect_tx(bar, (DH < 128 ? 1 : 2) * (uint32_t)L::VTILE);
           else remote_arrive(full_lead + (uint32_t)bf * 8u);
         }
         __syncwarp();
         bar = clear ? smem_u32(&v_own) : bar & LEADER_MASK;
-        if (lane < 2 * nb)
+        if (fetch && lane < 2 * nb)
           copy4d(dst + (uint32_t)blk * L::PIECE + (uint32_t)ch * L::KBLOCK + (uint32_t)pc * piece_bytes, &tmkv, row, u.hk * (DH / 64) + half * (DH / 128) + ch,
                  a.plane + 1, bar);
         if (clear) {
           wait_warp(bar, ph_own, wl);
           ph_own ^= 1u;
-          for (int i = lane; i < (clear_to - rem) * (DH / 16); i += 32) {              // (a row: 8 x 16 bytes in each of DH / 128 blocks)
-            const int r = rem + i / (DH / 16), c = i % (DH / 16);
+          for (int i = lane; i < (clear_to - rem) * (L::VN / 16); i += 32) {           // (a row: 8 x 16 bytes in each of VN / 128 blocks)
+            const int r = rem + i / (L::VN / 16), c = i % (L::VN / 16);
             asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(dst + (uint32_t)((r >> 6) * L::PIECE + (c >> 3) * L::KBLOCK + (r & 63) * 128 + (c & 7) * 16)), "r"(0u) : "memory");
           }
           fence_async_smem();                    // generic-proxy writes, read next by the tensor cores
@@ -464,7 +479,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
             }
             wait_warp(k_bar + 8u * rs.at, rs.parity, wc);
             tc_fence_after();
-            const uint64_t db = dk + (uint64_t)((uint32_t)rs.at * (L::TILE >> 4));      // (a 64-channel block further: 128 x 128 and 64 x 128 bytes)
+            const uint64_t db = dk + (uint64_t)((uint32_t)rs.at * (L::KTILE >> 4));      // (a 64-channel block further: 128 x 128 and 64 x 128 bytes)
 #pragma unroll
             for (int c = 0; c < DH / 64; ++c)
               umma2_ss_x4(tmem_s + (uint32_t)rs.at * KB, dq + (uint64_t)(c * ((128 * 128) >> 4)), db + (uint64_t)(c * (L::KBLOCK >> 4)), IDESC_S, c == 0 ? 1u : 0u, elected);
@@ -482,7 +497,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
             wait_warp(p_bar + 16u * rp.at + 8u * kh, rp.parity, wc);
             tc_fence_after();
             // A = P of this tile: bf16 pairs in the first 64 columns of its S buffer
-            umma2_ts_x4(tmem_o, tmem_s + (uint32_t)rp.at * KB + (uint32_t)kh * 32, dv + (uint64_t)((uint32_t)rp.at * (L::TILE >> 4) + kh * (L::PIECE >> 4)), IDESC_PV,
+            umma2_ts_x4(tmem_o, tmem_s + (uint32_t)rp.at * KB + (uint32_t)kh * 32, dv + (uint64_t)((uint32_t)rp.at * (L::VTILE >> 4) + kh * (L::PIECE >> 4)), IDESC_PV,
                         t == 0 && kh == 0 ? 1u : 0u, elected);
           }
           if (elected) umma2_commit(d_bar + 8u * rp.at);
@@ -603,16 +618,15 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
       for (Unit u = next_unit(k); u.r.b >= 0; u = next_unit(k)) {
         const int n_rows = min(TOK, u.r.n - u.tok0 - half * TOK) * G, end = min((u.t0 + u.T) * KB, u.r.kv);
         for (int rr = q * 32; rr < min(n_rows, q * 32 + 32); ++rr) {
-          constexpr int C = DH / 128;         // channels of a lane, of this warp's
           const int rt = rr / G, tok = u.r.lo + u.tok0 + half * TOK + rt, head = u.hk * G + rr - rt * G;
           const int lim = u.r.limit(u.tok0 + half * TOK + rt, 1);
           const size_t slot = ((size_t)u.range * a.pb.tokens + tok) * a.hq + head;
           __nv_bfloat16* ob = (__nv_bfloat16*)a.out + ((size_t)tok * a.hq + head) * DH + c0;
           float* of = a.part_o + slot * DH + c0;
           bool bad_row = false;
-          for (int e = 0; e < C; ++e) bad_row |= !(fabsf(u.ranges == 1 ? __bfloat162float(ob[lane * C + e]) : of[lane * C + e]) < INFINITY);
+          for (int e = lane; e < DH / 4; e += 32) bad_row |= !(fabsf(u.ranges == 1 ? __bfloat162float(ob[e]) : of[e]) < INFINITY);
           if (!__any_sync(0xffffffffu, bad_row)) continue;
-          if (!paged_hidden_odd<C, __nv_bfloat16>(a, u.r.b, u.hk, DH, c0, max(u.t0 * KB, lim), end)) continue;
+          if (!paged_hidden_odd<DH / 32, __nv_bfloat16>(a, u.r.b, u.hk, DH, 0, max(u.t0 * KB, lim), end)) continue;
           float o[DH / 32], M, sum;
           paged_row_alone<DH>(a, u.r.b, (const __nv_bfloat16*)a.q + tok * a.q_stride + (long long)head * DH, u.hk, u.t0 * KB, min(end, lim), o, M, sum);
           // (a key range's result is relative to the maximum that stands beside it)
@@ -680,23 +694,23 @@ cudaError_t launch_one(const PagedAttn& a, const phyai_paged_cache_t* cache, lon
   if (items < 1 || pairs < 1) return cudaErrorInvalidConfiguration;
   const int piece_shift = a.pb.page_shift < 6 ? a.pb.page_shift : 6;
   CUtensorMap tq, tkv;
-  if (!query_map(&tq, a, DH) || !paged_pool_map(&tkv, cache, 1u << piece_shift, piece_shift == 6 ? DH / 128 : 1)) return cudaErrorInvalidValue;
+  if (!query_map(&tq, a, DH) || !paged_pool_map(&tkv, cache, 1u << piece_shift, piece_shift == 6 ? PpLayout<DH>::VN / 128 : 1)) return cudaErrorInvalidValue;
   const unsigned grid = 2u * (unsigned)(items < pairs ? items : pairs);
   return launch_pdl(k_paged_pair<DH>, dim3(grid), dim3(PP_THREADS), PpLayout<DH>::SMEM, st, a, tq, tkv, piece_shift);
 }
 
 }  // namespace
 
-bool paged_pair_supported(int dh, int group) { return (dh == 128 || dh == 256) && group <= 128 && paged_pair_resident(dh) > 0; }
+bool paged_pair_supported(int dh, int group) { return (dh == 64 || dh == 128 || dh == 256) && group <= 128 && paged_pair_resident(dh) > 0; }
 int paged_pair_tokens(int group) { return 2 * (128 / group); }
 
 int paged_pair_resident(int dh) {
-  static PerDeviceCount resident[2];
-  return dh == 256 ? resident[1].get(resident_one<256>) : resident[0].get(resident_one<128>);
+  static PerDeviceCount resident[3];
+  return dh == 256 ? resident[2].get(resident_one<256>) : dh == 128 ? resident[1].get(resident_one<128>) : resident[0].get(resident_one<64>);
 }
 
 cudaError_t launch_paged_pair(const PagedAttn& a, const phyai_paged_cache_t* cache, long long items, cudaStream_t st) {
-  return cache->head_dim == 256 ? launch_one<256>(a, cache, items, st) : launch_one<128>(a, cache, items, st);
+  return cache->head_dim == 256 ? launch_one<256>(a, cache, items, st) : cache->head_dim == 128 ? launch_one<128>(a, cache, items, st) : launch_one<64>(a, cache, items, st);
 }
 
 }  // namespace phyai
