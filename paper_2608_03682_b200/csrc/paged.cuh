@@ -153,6 +153,7 @@ __host__ __device__ __forceinline__ int ranges_of(int tiles, int most, int least
 bool paged_pool_map(void* map, const phyai_paged_cache_t* c, uint32_t rows, uint32_t blocks);
 
 // many rows: paged_attention_pair.cu
+constexpr int PAGED_PAIR_MERGE = 7;                     // time that splitting units costs (fp32 results, a second kernel), in tiles of 128 keys
 bool paged_pair_supported(int dh, int group);
 int paged_pair_tokens(int group);                       // tokens of a unit
 int paged_pair_resident(int dh);                        // pairs at a time (0 on an error)

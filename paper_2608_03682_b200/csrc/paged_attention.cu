@@ -318,14 +318,15 @@ __global__ void __launch_bounds__(FW * 32, 2) k_paged_few(const PagedAttn a, con
 // fp32
 // =============================================================================================
 constexpr int XT = 128, XK = 32;         // threads; keys per tile
-constexpr int F32_LEAST = 2;             // tiles of keys in a range, at least
 
 // A thread takes RR rows and, of them, 4 of a tile's 32 logits and DH / 8 of the accumulator's channels; the 8 threads of a row are
-// neighbours in a warp, so that P and the statistics cross lanes by shuffles and a warp's own shared memory.
+// neighbours in a warp, so that P and the statistics cross lanes by shuffles and a warp's own shared memory.  The next tile's K is on its way
+// while P V of this one is computed, its V under the next logits; a tile's rows in the planes are looked up once, a tile ahead.
 template <int DH, int RR>
 __global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
   constexpr int RT = 16 * RR, PITCH = DH + 4, PP = XK + 4, CJ = DH / 32;
   extern __shared__ __align__(16) uint8_t smem_raw[];
+  __shared__ long long s_at[2][XK];        // element offset of a tile's keys in the planes, -1: none
   float* const Q = reinterpret_cast<float*>(smem_raw);
   float *const K = Q + RT * PITCH, *const V = K + XK * PITCH, *const P = V + XK * PITCH;
   const int tid = threadIdx.x, rg = tid >> 3, kg = tid & 7, lane = tid & 31, warp = tid >> 5;
@@ -342,9 +343,36 @@ __global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
   if (r.b < 0 || skip) return;
   const int rows = min(RT, r.n * a.group - tile * RT), row0 = tile * RT;
   const int n_keys = r.limit((row0 + rows - 1) / a.group, a.causal);
-  const int tiles = (n_keys + XK - 1) / XK, ranges = ranges_of(tiles, a.ranges, F32_LEAST), range = blockIdx.z;
+  const int tiles = (n_keys + XK - 1) / XK, ranges = ranges_of(tiles, a.ranges, 1), range = blockIdx.z;
   if (range >= ranges) return;
   const int t0 = (int)((long long)tiles * range / ranges), t1 = (int)((long long)tiles * (range + 1) / ranges);
+  bool bad_page = false;
+  auto look_up = [&](int kt) {
+    if (tid < XK && kt < t1) {
+      const int key = kt * XK + tid;
+      long long row = -1;
+      if (key < n_keys) {
+        row = paged_row(a.pb, r.b, key);
+        bad_page |= row < 0;
+      }
+      s_at[kt & 1][tid] = row < 0 ? -1 : (row * a.hkv + hk) * DH;
+    }
+  };
+  auto fetch = [&](int kt, const void* plane, float* dst) {
+    if (kt < t1) {
+#pragma unroll 8
+      for (int i = tid; i < XK * (DH / 4); i += XT) {
+        const int kr = i / (DH / 4), c = (i % (DH / 4)) * 4;
+        const long long at = s_at[kt & 1][kr];
+        cp_async16(smem_u32(dst + kr * PITCH + c), (const float*)plane + (at < 0 ? 0 : at + c), at < 0 ? 0u : 16u);
+      }
+    }
+    cp_async_commit();
+  };
+  look_up(t0);
+  __syncthreads();
+  fetch(t0, a.k_plane, K);
+  fetch(t0, a.v_plane, V);
   for (int i = tid; i < RT * (DH / 4); i += XT) {
     const int rr = i / (DH / 4), c = (i % (DH / 4)) * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -358,22 +386,10 @@ __global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
     const int rr = rg + 16 * i;
     m[i] = -INFINITY, lim[i] = rr < rows ? r.limit((row0 + rr) / a.group, a.causal) : n_keys;
   }
-  bool bad_page = false;
   for (int kt = t0; kt < t1; ++kt) {
-    __syncthreads();
-    for (int i = tid; i < 2 * XK * (DH / 4); i += XT) {
-      const int is_v = i >= XK * (DH / 4), j = i - is_v * XK * (DH / 4), kr = j / (DH / 4), c = (j % (DH / 4)) * 4, key = kt * XK + kr;
-      long long row = -1;
-      if (key < n_keys) {
-        row = paged_row(a.pb, r.b, key);
-        bad_page |= row < 0;
-      }
-      const float* src = (const float*)(is_v ? a.v_plane : a.k_plane);
-      cp_async16(smem_u32((is_v ? V : K) + kr * PITCH + c), row >= 0 ? src + ((size_t)row * a.hkv + hk) * DH + c : src, row >= 0 ? 16u : 0u);
-    }
-    cp_async_commit();
-    cp_async_wait<0>();
-    __syncthreads();
+    look_up(kt + 1);
+    cp_async_wait<1>();
+    __syncthreads();                       // K of this tile, Q
     float s[RR][4] = {};
 #pragma unroll 4
     for (int d = 0; d < DH; d += 4) {
@@ -387,6 +403,8 @@ __global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
         for (int j = 0; j < 4; ++j) s[i][j] = fmaf(qv.x, kv[j].x, fmaf(qv.y, kv[j].y, fmaf(qv.z, kv[j].z, fmaf(qv.w, kv[j].w, s[i][j]))));
       }
     }
+    __syncthreads();
+    fetch(kt + 1, a.k_plane, K);
 #pragma unroll
     for (int i = 0; i < RR; ++i) {
       float mx = -INFINITY;
@@ -411,7 +429,8 @@ __global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[i][j][e] *= corr;
     }
-    __syncwarp();
+    cp_async_wait<1>();
+    __syncthreads();                       // V of this tile
 #pragma unroll 2
     for (int k = 0; k < XK; k += 4) {
       float4 p[RR];
@@ -431,7 +450,10 @@ __global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
         }
       }
     }
+    __syncthreads();
+    fetch(kt + 1, a.v_plane, V);
   }
+  cp_async_wait<0>();
   if (bad_page) atomicExch(a.status, ST_INVALID_ARG);
 #pragma unroll
   for (int i = 0; i < RR; ++i) {
@@ -556,8 +578,10 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
     const int per = paged_pair_tokens(group), pairs = paged_pair_resident((int)c->head_dim);
     const long long full = (tokens + per - 1) / per > holders ? (tokens + per - 1) / per : holders;
     p.pair = 1, p.units = tokens / per + holders;
-    // key ranges where there are fewer units than one and a half rounds of the pairs (the kernel cuts them to equal pieces)
-    long long ranges = 2 * full * c->n_kv_heads < 3ll * pairs ? (3ll * pairs + full * c->n_kv_heads - 1) / (full * c->n_kv_heads) : 1;
+    // Key ranges where there are fewer units than one and a half rounds of the pairs, and where the time that splitting saves could be more than
+    // it costs (the kernel cuts the ranges by the lengths, or leaves the units whole: this is the same rule at the longest that they can be).
+    const long long u = full * c->n_kv_heads, tiles = (keys + 127) / 128, rounds = (u + pairs - 1) / pairs;
+    long long ranges = 2 * u < 3ll * pairs && tiles * (rounds * pairs - u) > (long long)PAGED_PAIR_MERGE * pairs ? (3ll * pairs + u - 1) / u : 1;
     if (ranges > keys / 256) ranges = keys / 256;
     p.ranges = (int)(ranges < 1 ? 1 : ranges > 64 ? 64 : ranges);
     return p;
@@ -569,10 +593,11 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
     p.rt = rows <= 8ll * holders ? 8 : 16;
   }
   p.units = rows / p.rt + holders;
-  // parts of a row tile's keys: enough blocks for two on each SM, of at least 128 keys; up to eight of them are a cluster
+  // parts of a row tile's keys: enough blocks for two on each SM, of at least 128 keys (fp32: a tile of 32); up to eight of them are a cluster
   const long long full = (rows + p.rt - 1) / p.rt > holders ? (rows + p.rt - 1) / p.rt : holders, blocks = full * c->n_kv_heads;
   long long parts = (2ll * n_sm + blocks - 1) / blocks;
-  if (parts > keys / 128) parts = keys / 128;
+  const int least = p.f32 ? 32 : 128;
+  if (parts > keys / least) parts = keys / least;
   if (!p.f32)
     while (p.csize < 8 && 2 * p.csize <= parts) p.csize *= 2;
   parts /= p.csize;

@@ -30,7 +30,6 @@ namespace {
 
 constexpr int KB = 128;                        // keys per tile: two blocks of 64
 constexpr int PP_THREADS = 20 * 32;
-constexpr int PAIR_MERGE = 7;                  // tiles' time that splitting units costs
 constexpr int PAIR_LEAST = 2;                  // tiles of keys in a range where units are split, at least
 
 // head_dim 64: V counts as 128 channels, of which the second CTA's half is zero and never fetched (half of 64 channels would be 64 bytes a
@@ -272,9 +271,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     __syncthreads();
     const long long pieces = 2ll * n_pairs - (long long)units * a.hkv / 2, per = pieces > 0 ? (tiles * a.hkv + pieces - 1) / pieces : 0x7fffffff;
     longest = (int)(per < PAIR_LEAST ? PAIR_LEAST : per > 0x7fffffff ? 0x7fffffff : per);
-    // (fp32 results and the second kernel cost what PAIR_MERGE tiles do: not where the longest units, left whole, end before that)
+    // (fp32 results and the second kernel cost what PAGED_PAIR_MERGE tiles do: not where the longest units, left whole, end before that)
     const long long whole = (long long)most * (((long long)units * a.hkv + n_pairs - 1) / n_pairs);
-    if (whole <= tiles * a.hkv / n_pairs + PAIR_MERGE) longest = 0x7fffffff;
+    if (whole <= tiles * a.hkv / n_pairs + PAGED_PAIR_MERGE) longest = 0x7fffffff;
   }
   auto ranges_for = [&](int kv) { return a.ranges > 1 ? min(a.ranges, max(1, ((kv + KB - 1) / KB - 1) / longest + 1)) : 1; };
   int acc = 0;                                      // key ranges of units (of one kv head) so far
