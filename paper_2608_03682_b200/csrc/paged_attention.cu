@@ -317,19 +317,20 @@ __global__ void __launch_bounds__(FW * 32, 2) k_paged_few(const PagedAttn a, con
 // =============================================================================================
 // fp32
 // =============================================================================================
-constexpr int XT = 128, XK = 32;         // threads; keys per tile
+constexpr int XK = 32;                   // keys per tile
 
-// A thread takes RR rows and, of them, 4 of a tile's 32 logits and DH / 8 of the accumulator's channels; the 8 threads of a row are
-// neighbours in a warp, so that P and the statistics cross lanes by shuffles and a warp's own shared memory.  The next tile's K is on its way
-// while P V of this one is computed, its V under the next logits; a tile's rows in the planes are looked up once, a tile ahead.
-template <int DH, int RR>
-__global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
-  constexpr int RT = 16 * RR, PITCH = DH + 4, PP = XK + 4, CJ = DH / 32;
+// A warp takes RW rows, a block NW warps.  Logits: a lane takes one of a tile's 32 keys, so that a load of K is read by all lanes at full width and the queries'
+// are broadcasts (with 8 keys a load, repeated for 4 rows, shared memory bounded the kernel at a third of the rate); P V: a lane takes DH / 32
+// channels, P are the broadcasts.  The next tile's K is on its way while P V of this one is computed, its V under the next logits; a tile's
+// rows in the planes are looked up once, a tile ahead.
+template <int DH, int RW, int NW>
+__global__ void __launch_bounds__(NW * 32) k_paged_f32(const PagedAttn a) {
+  constexpr int XT = NW * 32, RT = NW * RW, PITCH = DH + 4, PP = XK + 4, C = DH / 32, CV = C < 4 ? C : 4, CJ = C / CV, RB = RW < 4 ? RW : 4;
   extern __shared__ __align__(16) uint8_t smem_raw[];
   __shared__ long long s_at[2][XK];        // element offset of a tile's keys in the planes, -1: none
   float* const Q = reinterpret_cast<float*>(smem_raw);
   float *const K = Q + RT * PITCH, *const V = K + XK * PITCH, *const P = V + XK * PITCH;
-  const int tid = threadIdx.x, rg = tid >> 3, kg = tid & 7, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int hk = blockIdx.y;
   pdl_launch_dependents();
   pdl_wait();
@@ -379,75 +380,64 @@ __global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
     if (rr < rows) v = *reinterpret_cast<const float4*>((const float*)a.q + (r.lo + (row0 + rr) / a.group) * a.q_stride + (long long)(hk * a.group + (row0 + rr) % a.group) * DH + c);
     *reinterpret_cast<float4*>(Q + rr * PITCH + c) = v;
   }
-  float acc[RR][CJ][4] = {}, m[RR], l[RR] = {};
-  int lim[RR];
+  const int wr = warp * RW;                // first row of this warp
+  float acc[RW][C] = {}, m[RW], l[RW] = {};            // l: of this lane's keys
+  int lim[RW];
 #pragma unroll
-  for (int i = 0; i < RR; ++i) {
-    const int rr = rg + 16 * i;
-    m[i] = -INFINITY, lim[i] = rr < rows ? r.limit((row0 + rr) / a.group, a.causal) : n_keys;
-  }
+  for (int i = 0; i < RW; ++i) m[i] = -INFINITY, lim[i] = wr + i < rows ? r.limit((row0 + wr + i) / a.group, a.causal) : n_keys;
   for (int kt = t0; kt < t1; ++kt) {
     look_up(kt + 1);
     cp_async_wait<1>();
     __syncthreads();                       // K of this tile, Q
-    float s[RR][4] = {};
+    float s[RW] = {};
 #pragma unroll 4
     for (int d = 0; d < DH; d += 4) {
-      float4 kv[4];
+      const float4 k = *reinterpret_cast<const float4*>(K + lane * PITCH + d);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4*>(K + (kg + 8 * j) * PITCH + d);
-#pragma unroll
-      for (int i = 0; i < RR; ++i) {
-        const float4 qv = *reinterpret_cast<const float4*>(Q + (rg + 16 * i) * PITCH + d);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[i][j] = fmaf(qv.x, kv[j].x, fmaf(qv.y, kv[j].y, fmaf(qv.z, kv[j].z, fmaf(qv.w, kv[j].w, s[i][j]))));
+      for (int i = 0; i < RW; ++i) {
+        const float4 q = *reinterpret_cast<const float4*>(Q + (wr + i) * PITCH + d);
+        s[i] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, s[i]))));
       }
     }
     __syncthreads();
     fetch(kt + 1, a.k_plane, K);
 #pragma unroll
-    for (int i = 0; i < RR; ++i) {
-      float mx = -INFINITY;
+    for (int i = 0; i < RW; ++i) {
+      s[i] = kt * XK + lane < lim[i] ? s[i] * a.scale_log2 : -INFINITY;
+      const float mn = fmaxf(m[i], warp_max(s[i])), sub = mn == -INFINITY ? 0.f : mn, p = exp2f(s[i] - sub);
+      P[(wr + i) * PP + lane] = p;
+      if (mn != m[i]) {                    // (the same in all lanes)
+        const float corr = exp2f(m[i] - sub);
+        l[i] *= corr, m[i] = mn;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        s[i][j] = kt * XK + kg + 8 * j < lim[i] ? s[i][j] * a.scale_log2 : -INFINITY;
-        mx = fmaxf(mx, s[i][j]);
+        for (int e = 0; e < C; ++e) acc[i][e] *= corr;
       }
-#pragma unroll
-      for (int o = 1; o < 8; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-      const float mn = fmaxf(m[i], mx), sub = mn == -INFINITY ? 0.f : mn, corr = exp2f(m[i] - sub);
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float p = exp2f(s[i][j] - sub);
-        P[(rg + 16 * i) * PP + kg + 8 * j] = p;
-        sum += p;
-      }
-      l[i] = l[i] * corr + sum, m[i] = mn;
-#pragma unroll
-      for (int j = 0; j < CJ; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] *= corr;
+      l[i] += p;
     }
     cp_async_wait<1>();
     __syncthreads();                       // V of this tile
-#pragma unroll 2
+#pragma unroll 1
     for (int k = 0; k < XK; k += 4) {
-      float4 p[RR];
+      float v[4][C];
 #pragma unroll
-      for (int i = 0; i < RR; ++i) p[i] = *reinterpret_cast<const float4*>(P + (rg + 16 * i) * PP + k);
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
+      for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
         for (int j = 0; j < CJ; ++j) {
-          const float4 v = *reinterpret_cast<const float4*>(V + (k + kk) * PITCH + kg * 4 + 32 * j);
-#pragma unroll
-          for (int i = 0; i < RR; ++i) {
-            const float w = kk == 0 ? p[i].x : kk == 1 ? p[i].y : kk == 2 ? p[i].z : p[i].w;
-            acc[i][j][0] = fmaf(w, v.x, acc[i][j][0]), acc[i][j][1] = fmaf(w, v.y, acc[i][j][1]);
-            acc[i][j][2] = fmaf(w, v.z, acc[i][j][2]), acc[i][j][3] = fmaf(w, v.w, acc[i][j][3]);
-          }
+          const float* src = V + (k + kk) * PITCH + lane * CV + 32 * CV * j;
+          if constexpr (CV == 4) *reinterpret_cast<float4*>(&v[kk][4 * j]) = *reinterpret_cast<const float4*>(src);
+          else *reinterpret_cast<float2*>(&v[kk][2 * j]) = *reinterpret_cast<const float2*>(src);
         }
+#pragma unroll
+      for (int i0 = 0; i0 < RW; i0 += RB) {
+        float p[RB][4];
+#pragma unroll
+        for (int i = 0; i < RB; ++i) *reinterpret_cast<float4*>(p[i]) = *reinterpret_cast<const float4*>(P + (wr + i0 + i) * PP + k);
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int e = 0; e < C; ++e) acc[i0 + i][e] = fmaf(p[i][kk], v[kk][e], acc[i0 + i][e]);
       }
     }
     __syncthreads();
@@ -456,39 +446,34 @@ __global__ void __launch_bounds__(XT) k_paged_f32(const PagedAttn a) {
   cp_async_wait<0>();
   if (bad_page) atomicExch(a.status, ST_INVALID_ARG);
 #pragma unroll
-  for (int i = 0; i < RR; ++i) {
-    const int rr = rg + 16 * i;
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+  for (int i = 0; i < RW; ++i) {
+    if (wr + i >= rows) continue;          // (the whole warp)
+    const float sum = warp_sum(l[i]);
+    const int it = (row0 + wr + i) / a.group, tok = r.lo + it, h = hk * a.group + (row0 + wr + i) % a.group;
+    const size_t slot = ((size_t)range * a.pb.tokens + tok) * a.hq + h;
+    float* const dst = ranges == 1 ? (float*)a.out + ((size_t)tok * a.hq + h) * DH : a.part_o + slot * DH;
+    const float inv = ranges > 1 ? 1.0f : sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
     float fin = 0.f;
 #pragma unroll
-    for (int j = 0; j < CJ; ++j) fin += fabsf(acc[i][j][0]) + fabsf(acc[i][j][1]) + fabsf(acc[i][j][2]) + fabsf(acc[i][j][3]);
-    const unsigned odd = __ballot_sync(0xffffffffu, a.causal && rr < rows && !(fin < INFINITY));     // (see k_paged_few)
-    const int tok = r.lo + (row0 + rr) / a.group, h = hk * a.group + (row0 + rr) % a.group;
-    const size_t slot = ((size_t)range * a.pb.tokens + tok) * a.hq + h;
-    if (rr < rows) {
-      float* dst = ranges == 1 ? (float*)a.out + ((size_t)tok * a.hq + h) * DH : a.part_o + slot * DH;
-      const float inv = ranges > 1 ? 1.0f : l[i] > 0.f || l[i] != l[i] ? 1.0f / l[i] : 0.f;
+    for (int j = 0; j < CJ; ++j) {
+      float o[CV];
 #pragma unroll
-      for (int j = 0; j < CJ; ++j)
-        *reinterpret_cast<float4*>(dst + kg * 4 + 32 * j) = make_float4(acc[i][j][0] * inv, acc[i][j][1] * inv, acc[i][j][2] * inv, acc[i][j][3] * inv);
-      if (kg == 0 && a.ranges > 1) a.part_ml[slot] = make_float4(m[i], l[i], (float)ranges, 0.f);
+      for (int e = 0; e < CV; ++e) o[e] = acc[i][CV * j + e] * inv, fin = fmaf(acc[i][CV * j + e], 0.f, fin);
+      if constexpr (CV == 4) *reinterpret_cast<float4*>(dst + lane * 4 + 128 * j) = make_float4(o[0], o[1], o[2], o[3]);
+      else *reinterpret_cast<float2*>(dst + lane * 2 + 64 * j) = make_float2(o[0], o[1]);
     }
-    __syncwarp();
-    for (int z = 0; z < 4; ++z) {                        // the four rows of this warp
-      if (!(odd & (0xffu << (8 * z)))) continue;
-      const int r2 = warp * 4 + z + 16 * i, i2 = (row0 + r2) / a.group;
-      if (!paged_hidden_odd<DH / 32, float>(a, r.b, hk, DH, 0, max(t0 * XK, r.limit(i2, 1)), min(t1 * XK, n_keys))) continue;
-      const int tok2 = r.lo + i2, h2 = hk * a.group + (row0 + r2) % a.group;
-      float o[DH / 32], M, sum;
-      paged_row_alone<DH>(a, r.b, (const float*)a.q + tok2 * a.q_stride + (long long)h2 * DH, hk, t0 * XK, min(t1 * XK, r.limit(i2, 1)), o, M, sum);
-      const size_t slot2 = ((size_t)range * a.pb.tokens + tok2) * a.hq + h2;
-      float* dst = (ranges == 1 ? (float*)a.out + ((size_t)tok2 * a.hq + h2) * DH : a.part_o + slot2 * DH) + lane * (DH / 32);
-      const float inv = ranges > 1 ? 1.0f : sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+    if (lane == 0 && a.ranges > 1) a.part_ml[slot] = make_float4(m[i], sum, (float)ranges, 0.f);
+    // (0 x infinity and 0 x NaN: see k_paged_few)
+    if (!a.causal || __all_sync(0xffffffffu, fin == 0.f)) continue;
+    const int lm = r.limit(it, 1);
+    if (!paged_hidden_odd<DH / 32, float>(a, r.b, hk, DH, 0, max(t0 * XK, lm), min(t1 * XK, n_keys))) continue;
+    float o[DH / 32], M, sm;
+    paged_row_alone<DH>(a, r.b, (const float*)a.q + tok * a.q_stride + (long long)h * DH, hk, t0 * XK, min(t1 * XK, lm), o, M, sm);
+    const float w = ranges > 1 ? 1.0f : sm > 0.f || sm != sm ? 1.0f / sm : 0.f;
+    __syncwarp();                          // (behind the stores above, of other lanes)
 #pragma unroll
-      for (int e = 0; e < DH / 32; ++e) dst[e] = o[e] * inv;
-      if (lane == 0 && ranges > 1) a.part_ml[slot2] = make_float4(M, sum, (float)ranges, 0.f);
-    }
+    for (int e = 0; e < DH / 32; ++e) dst[lane * (DH / 32) + e] = o[e] * w;
+    if (lane == 0 && ranges > 1) a.part_ml[slot] = make_float4(M, sm, (float)ranges, 0.f);
   }
 }
 
@@ -588,15 +573,16 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
   }
   if (p.f32) {
     // tiles of 64 rows where there are enough of them for the SMs (17 tokens of 4 heads of 4 requests: 16-row tiles)
-    p.rt = rows / 64 * c->n_kv_heads >= n_sm ? 64 : 16;
+    p.rt = rows / 64 * c->n_kv_heads >= n_sm ? 64 : rows <= 4ll * holders ? 4 : rows <= 8ll * holders ? 8 : 16;
   } else {
     p.rt = rows <= 8ll * holders ? 8 : 16;
   }
   p.units = rows / p.rt + holders;
-  // parts of a row tile's keys: enough blocks for two on each SM, of at least 128 keys (fp32: a tile of 32); up to eight of them are a cluster
+  // parts of a row tile's keys: enough blocks for two on each SM, of at least 128 keys; up to eight of them are a cluster.  fp32: five, of at
+  // least a tile of 32 (two: 1.5 times the time with one token a request)
   const long long full = (rows + p.rt - 1) / p.rt > holders ? (rows + p.rt - 1) / p.rt : holders, blocks = full * c->n_kv_heads;
-  long long parts = (2ll * n_sm + blocks - 1) / blocks;
   const int least = p.f32 ? 32 : 128;
+  long long parts = ((p.f32 ? 5ll : 2ll) * n_sm + blocks - 1) / blocks;
   if (parts > keys / least) parts = keys / least;
   if (!p.f32)
     while (p.csize < 8 && 2 * p.csize <= parts) p.csize *= 2;
@@ -628,16 +614,16 @@ cudaError_t launch_few(const PagedAttn& a, const Plan& p, const CUtensorMap& map
   cfg.attrs = at, cfg.numAttrs = p.csize > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, k_paged_few<DH, NT>, a, map, p.csize);
 }
-template <int DH, int RR>
+template <int DH, int RW, int NW>
 cudaError_t launch_f32(const PagedAttn& a, const Plan& p, cudaStream_t st) {
-  constexpr size_t smem = ((size_t)(16 * RR + 2 * XK) * (DH + 4) + 16 * RR * (XK + 4)) * 4;
+  constexpr size_t smem = ((size_t)(NW * RW + 2 * XK) * (DH + 4) + NW * RW * (XK + 4)) * 4;
   static PerDeviceOnce once;
   if (once.needed()) {
-    const cudaError_t e = allow_smem(k_paged_f32<DH, RR>, smem);
+    const cudaError_t e = allow_smem(k_paged_f32<DH, RW, NW>, smem);
     if (e != cudaSuccess) return e;
     once.done();
   }
-  return launch_pdl(k_paged_f32<DH, RR>, dim3((unsigned)p.units, a.hkv, p.ranges), dim3(XT), smem, st, a);
+  return launch_pdl(k_paged_f32<DH, RW, NW>, dim3((unsigned)p.units, a.hkv, p.ranges), dim3(NW * 32), smem, st, a);
 }
 }  // namespace
 
@@ -703,9 +689,9 @@ phyai_status_t phyai_paged_attention(const phyai_paged_cache_t* cache, uint32_t 
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaErrorInvalidValue;
   if (p.f32) {
-    if (dh == 64) e = p.rt == 16 ? launch_f32<64, 1>(a, p, st) : launch_f32<64, 4>(a, p, st);
-    else if (dh == 128) e = p.rt == 16 ? launch_f32<128, 1>(a, p, st) : launch_f32<128, 4>(a, p, st);
-    else e = p.rt == 16 ? launch_f32<256, 1>(a, p, st) : launch_f32<256, 4>(a, p, st);
+#define PHYAI_F32_ROWS(DH) (p.rt == 4 ? launch_f32<DH, 1, 4>(a, p, st) : p.rt == 8 ? launch_f32<DH, 1, 8>(a, p, st) : p.rt == 16 ? launch_f32<DH, 2, 8>(a, p, st) : launch_f32<DH, 8, 8>(a, p, st))
+    e = dh == 64 ? PHYAI_F32_ROWS(64) : dh == 128 ? PHYAI_F32_ROWS(128) : PHYAI_F32_ROWS(256);
+#undef PHYAI_F32_ROWS
   } else if (p.pair) {
     e = launch_paged_pair(a, cache, p.units * a.hkv * p.ranges, st);
   } else {
