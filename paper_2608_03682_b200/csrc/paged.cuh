@@ -69,28 +69,35 @@ __device__ __forceinline__ bool paged_unit(const PagedAttn& a, int unit, PagedRe
   bool bad = false;
   int acc = 0;
   r.b = -1, r.lo = r.n = r.kv = r.prefix = 0, tile = 0;
-  for (int i0 = 0; i0 < a.pb.batch; i0 += 32) {
-    const int i = i0 + lane;
-    int lo = 0, hi = 0, kv = 0;
-    if (i < a.pb.batch) {
-      lo = a.pb.cu[i], hi = a.pb.cu[i + 1], kv = a.pb.kv_lens[i];
-      bad |= paged_entry_bad(a.pb, i, lo, hi, kv, false);
-    }
-    const int n = bad ? 0 : ((hi - lo) * a.group + RT - 1) / RT;
-    int incl = n;
+  for (int i0 = 0; i0 < a.pb.batch; i0 += 128) {      // (128 requests' lengths on their way at a time)
+    int lo[4], hi[4], kv[4];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += up;
+    for (int j = 0; j < 4; ++j) {
+      const int i = i0 + 32 * j + lane;
+      lo[j] = hi[j] = kv[j] = 0;
+      if (i < a.pb.batch) lo[j] = a.pb.cu[i], hi[j] = a.pb.cu[i + 1], kv[j] = a.pb.kv_lens[i];
     }
-    const unsigned hit = __ballot_sync(0xffffffffu, acc + incl > unit);
-    if (r.b < 0 && hit) {
-      const int src = __ffs(hit) - 1;
-      r.b = i0 + src, r.lo = __shfl_sync(0xffffffffu, lo, src), r.n = __shfl_sync(0xffffffffu, hi, src) - r.lo;
-      r.kv = __shfl_sync(0xffffffffu, kv, src);
-      tile = unit - acc - __shfl_sync(0xffffffffu, incl - n, src);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i0 + 32 * j >= a.pb.batch) break;
+      const bool wrong = i0 + 32 * j + lane < a.pb.batch && paged_entry_bad(a.pb, i0 + 32 * j + lane, lo[j], hi[j], kv[j], false);
+      bad |= wrong;
+      const int n = wrong ? 0 : ((hi[j] - lo[j]) * a.group + RT - 1) / RT;
+      int incl = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += up;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, acc + incl > unit);
+      if (r.b < 0 && hit) {
+        const int src = __ffs(hit) - 1;
+        r.b = i0 + 32 * j + src, r.lo = __shfl_sync(0xffffffffu, lo[j], src), r.n = __shfl_sync(0xffffffffu, hi[j], src) - r.lo;
+        r.kv = __shfl_sync(0xffffffffu, kv[j], src);
+        tile = unit - acc - __shfl_sync(0xffffffffu, incl - n, src);
+      }
+      acc += __shfl_sync(0xffffffffu, incl, 31);
     }
-    acc += __shfl_sync(0xffffffffu, incl, 31);
   }
   if (__any_sync(0xffffffffu, bad)) return false;
   if (r.b >= 0 && a.prefix_lens) r.prefix = min(max(a.prefix_lens[r.b], 0), r.kv);

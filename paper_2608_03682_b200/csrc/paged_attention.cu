@@ -2,7 +2,7 @@
 // merge of key ranges.
 //
 // Row (token i, head h) of a request sees keys [0, limit(i)); o = sum_k p_k v_k / sum_k p_k, p_k = 2^(scale log2(e) (q k_k - max)).
-// Statistics and accumulators are fp32; P is rounded to bf16 (2^-9 of each weight, below the rounding of the bf16 output's terms) because
+// Statistics and accumulators are fp32; P is rounded to bf16 (off by at most 2^-8 of each weight, as V itself is) because
 // it is an operand of the tensor cores; the fp32 cache keeps everything fp32.
 //
 // Few rows (one token of a request is `group` rows): the cache is read once and nothing is reused, so memory bounds it.  Every warp
@@ -665,6 +665,7 @@ phyai_status_t phyai_paged_attention(const phyai_paged_cache_t* cache, uint32_t 
   if (q_stride < (uint64_t)n_q_heads * cache->head_dim || q_stride > (1ull << 40)) return bad_arg("a row stride is smaller than the row's heads, or too large");
   if (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(workspace)) & 15u) || (q_stride * es) % 16)
     return bad_arg("pointers and row strides must be multiples of 16 bytes");
+  if (((reinterpret_cast<uintptr_t>(status_word) | reinterpret_cast<uintptr_t>(prefix_lens)) & 3u)) return bad_arg("status_word and prefix_lens must be 4-byte aligned");
   if ((uint64_t)tokens * (n_q_heads / cache->n_kv_heads) > 0x7fffffffull) return bad_arg("tokens too large");
   if (!tokens) return PHYAI_OK;
   const int n_sm = paged_sm_count();

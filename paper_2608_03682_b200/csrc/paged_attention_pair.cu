@@ -44,7 +44,10 @@ struct PpLayout {
   static constexpr int QTILE = 128 * DH * 2;
   static constexpr int STG = 1024;                           // output staging of a warp: 32 rows x 16 columns
   static constexpr int NB = (512 - VN) / 128;                // buffers of logits: what the accumulator leaves of the 512 columns
-  static constexpr size_t SMEM = 1024 + NB * (size_t)(KTILE + VTILE) + QTILE + 16 * STG;
+  static constexpr size_t USED = 1024 + NB * (size_t)(KTILE + VTILE) + QTILE + 16 * STG;
+  // One CTA an SM, and no other kernel that could wait there for tensor memory: two pairs of different kernels, each with tensor memory
+  // on one SM and waiting for the other's, would wait for good.
+  static constexpr size_t SMEM = USED > 209 * 1024 ? USED : 209 * 1024;
 };
 
 __device__ __forceinline__ void copy4d(uint32_t dst, const CUtensorMap* map, int c1, int c2, int c3, uint32_t bar) {

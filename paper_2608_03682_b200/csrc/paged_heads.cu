@@ -243,8 +243,8 @@ cudaError_t dispatch_heads(int dh, uint32_t in, uint32_t out, const HeadsArgs& a
   return cudaErrorInvalidValue;
 }
 
-// Pages -> packed rows.  Blocks move 16 KB of one plane (grid.y) and request (grid.z), four 16-byte loads a thread; every block adds up
-// the lengths before its request itself.
+// Pages -> packed rows.  Blocks move 16 KB of one plane (grid.y) and request (grid.z) at a time, four 16-byte loads a thread, every gridDim.x-th
+// chunk; every block adds up the lengths before its request itself, the loads of its first chunk on their way.
 constexpr int PP_T = 256, PP_U = 4, PP_CHUNK = PP_T * PP_U;
 __global__ void __launch_bounds__(PP_T) k_pack_pages(const uint4* pages, uint4* dst, int* cu, int* status, const PagedBatch p, long long kv_tokens,
                                                      int row_chunks) {
@@ -257,7 +257,6 @@ __global__ void __launch_bounds__(PP_T) k_pack_pages(const uint4* pages, uint4* 
   const int my_len = p.kv_lens[b];
   const bool first = blockIdx.x == 0 && blockIdx.y == 0;
   const int page_chunks = row_chunks << p.page_shift;
-  const int i0 = (int)blockIdx.x * PP_CHUNK + tid;
   const bool in_range = my_len >= 0 && (long long)my_len <= ((long long)p.max_pages << p.page_shift);
   const int n = in_range ? my_len * row_chunks : 0;
   if ((int)blockIdx.x * PP_CHUNK >= n && !first) return;
@@ -265,17 +264,21 @@ __global__ void __launch_bounds__(PP_T) k_pack_pages(const uint4* pages, uint4* 
   const uint4* src = pages + (size_t)blockIdx.y * plane_chunks;
   uint4 x[PP_U];
   bool have[PP_U], bad_page = false;
+  auto load = [&](long long i0) {
 #pragma unroll
-  for (int u = 0; u < PP_U; ++u) {
-    const int i = i0 + u * PP_T;
-    have[u] = false;
-    if (i < n) {
-      const int pg = i / page_chunks, page = p.table[(size_t)b * p.max_pages + pg];
-      have[u] = (unsigned)page < (unsigned)p.n_pages;
-      bad_page |= !have[u];
-      if (have[u]) x[u] = __ldcs(src + (size_t)page * page_chunks + (i - pg * page_chunks));
+    for (int u = 0; u < PP_U; ++u) {
+      const long long i = i0 + u * PP_T;
+      have[u] = false;
+      if (i < n) {
+        const int pg = (int)i / page_chunks, page = p.table[(size_t)b * p.max_pages + pg];
+        have[u] = (unsigned)page < (unsigned)p.n_pages;
+        bad_page |= !have[u];
+        if (have[u]) x[u] = __ldcs(src + (size_t)page * page_chunks + ((int)i - pg * page_chunks));
+      }
     }
-  }
+  };
+  long long i0 = (long long)blockIdx.x * PP_CHUNK + tid;
+  load(i0);
   // ---- rows before this request, all rows
   long long before = 0, total = 0;
   bool bad = false;
@@ -300,11 +303,16 @@ __global__ void __launch_bounds__(PP_T) k_pack_pages(const uint4* pages, uint4* 
     if (bad) atomicExch(status, ST_INVALID_ARG);
   }
   if (bad) return;
-  if (bad_page) atomicExch(status, ST_INVALID_ARG);
-  uint4* o = dst + ((size_t)blockIdx.y * kv_tokens + before) * row_chunks + i0;
+  uint4* const o = dst + ((size_t)blockIdx.y * kv_tokens + before) * row_chunks;
+  for (;;) {
 #pragma unroll
-  for (int u = 0; u < PP_U; ++u)
-    if (have[u]) o[u * PP_T] = x[u];
+    for (int u = 0; u < PP_U; ++u)
+      if (have[u]) o[i0 + u * PP_T] = x[u];
+    i0 += (long long)gridDim.x * PP_CHUNK;
+    if (i0 - tid >= n) break;
+    load(i0);
+  }
+  if (bad_page) atomicExch(status, ST_INVALID_ARG);
 }
 
 phyai_status_t bad_arg(const char* m) {
@@ -318,6 +326,7 @@ phyai_status_t launch_result(cudaError_t e) {
   return PHYAI_ERR_CUDA;
 }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 phyai_status_t check_heads(const phyai_heads_desc_t* d, uint32_t tokens, const void* q, uint64_t q_stride, const void* k, uint64_t k_stride,
                            const float* rope, uint64_t n_positions, const float* q_gain, const float* k_gain, const void* q_out,
@@ -342,6 +351,7 @@ phyai_status_t check_heads(const phyai_heads_desc_t* d, uint32_t tokens, const v
   if (!aligned16(q) || !aligned16(k) || !aligned16(rope) || !aligned16(q_gain) || !aligned16(k_gain) || !aligned16(q_out) ||
       (q && (q_stride * es) % 16) || (k_stride * es) % 16)
     return bad_arg("pointers and row strides must be multiples of 16 bytes");
+  if (!aligned4(status_word)) return bad_arg("status_word must be 4-byte aligned");
   if (rope && (n_positions == 0 || n_positions > 0x7fffffffull)) return bad_arg("n_positions out of range");
   return PHYAI_OK;
 }
@@ -379,6 +389,7 @@ phyai_status_t check_paged(const phyai_paged_cache_t* c, uint32_t layer, uint32_
   if (!all_layers && layer >= c->n_layers) return bad_arg("layer out of range");
   if (!batch || batch > (uint32_t)PAGED_MAX_BATCH) return bad_arg("batch must be 1..1024");
   if ((!all_layers && !cu) || !kv_lens || !table || !max_pages) return bad_arg("cu_q_lens, kv_lens or page_table is NULL, or max_pages is 0");
+  if (!aligned4(cu) || !aligned4(kv_lens) || !aligned4(table)) return bad_arg("cu_q_lens, kv_lens and page_table must be 4-byte aligned");
   if (tokens > 0x7fffffffu || (uint64_t)max_pages * c->page_size > 0x7fffffffull) return bad_arg("tokens or max_pages too large");
   out->cu = cu, out->kv_lens = kv_lens, out->table = table, out->batch = (int)batch, out->tokens = (int)tokens, out->max_pages = (int)max_pages;
   out->page_shift = __builtin_ctz(c->page_size), out->n_pages = (int)c->n_pages;
@@ -398,7 +409,7 @@ phyai_status_t phyai_norm_rope_heads(const phyai_heads_desc_t* desc, uint32_t to
   phyai_status_t s = check_heads(desc, tokens, q, q_stride, k, k_stride, rope_cos_sin, n_positions, q_gain, k_gain, q_out, status_word);
   if (s != PHYAI_OK) return s;
   if (tokens && (!k_out || (rope_cos_sin && !positions))) return bad_arg("k_out is NULL, or positions is NULL with a rotation");
-  if (!aligned16(k_out)) return bad_arg("pointers and row strides must be multiples of 16 bytes");
+  if (!aligned16(k_out) || !aligned4(positions)) return bad_arg("pointers and row strides must be multiples of 16 bytes, positions of 4");
   if (!tokens) return PHYAI_OK;
   HeadsArgs a = heads_args(desc, tokens, q, q_stride, k, k_stride, positions, rope_cos_sin, n_positions, q_gain, k_gain, q_out, status_word);
   a.k_out = k_out;
@@ -421,7 +432,7 @@ phyai_status_t phyai_append_paged_kv(const phyai_paged_cache_t* cache, const phy
   const uint64_t es = desc->in_dtype == PHYAI_F32 ? 4 : 2;
   if (tokens && !v) return bad_arg("a pointer argument is NULL");
   if (v_stride < (uint64_t)desc->n_kv_heads * desc->head_dim || v_stride > (1ull << 40)) return bad_arg("a row stride is smaller than the row's heads, or too large");
-  if (!aligned16(v) || (v_stride * es) % 16) return bad_arg("pointers and row strides must be multiples of 16 bytes");
+  if (!aligned16(v) || (v_stride * es) % 16 || !aligned4(positions)) return bad_arg("pointers and row strides must be multiples of 16 bytes, positions of 4");
   if (!tokens) return PHYAI_OK;
   a.v = v, a.v_stride = (long long)v_stride;
   const size_t plane = (size_t)cache->n_pages * cache->page_size * cache->n_kv_heads * cache->head_dim * (cache->dtype == PHYAI_F32 ? 4 : 2);
@@ -437,11 +448,13 @@ phyai_status_t phyai_pack_paged_kv(const phyai_paged_cache_t* cache, uint32_t ba
   phyai_status_t s = check_paged(cache, 0, batch, nullptr, kv_lens, page_table, max_pages, 0, true, &p);
   if (s != PHYAI_OK) return s;
   if ((!prefix_kv && kv_tokens) || !cu_prefix_lens || !status_word) return bad_arg("a pointer argument is NULL");
-  if (!aligned16(prefix_kv)) return bad_arg("prefix_kv must be 16-byte aligned");
+  if (!aligned16(prefix_kv) || !aligned4(cu_prefix_lens) || !aligned4(status_word)) return bad_arg("prefix_kv must be 16-byte aligned, cu_prefix_lens and status_word 4-byte");
   const size_t row_bytes = (size_t)cache->n_kv_heads * cache->head_dim * (cache->dtype == PHYAI_F32 ? 4 : 2), chunks = row_bytes / 16;
   const size_t longest = (size_t)max_pages * cache->page_size < kv_tokens ? (size_t)max_pages * cache->page_size : kv_tokens;
   if (kv_tokens > 0x7fffffffull || (size_t)max_pages * cache->page_size * chunks > 0x7fffffffull) return bad_arg("kv_tokens or max_pages too large");
-  const size_t gx = (longest * chunks + PP_CHUNK - 1) / PP_CHUNK;
+  // (a block per chunk of a request of twice the average length; the blocks of longer ones take several: a table is as wide as the longest
+  // request may become, and blocks without work are not free)
+  const size_t likely = 2 * kv_tokens / batch + 64, gx = ((longest < likely ? longest : likely) * chunks + PP_CHUNK - 1) / PP_CHUNK;
   return launch_result(launch_pdl(k_pack_pages, dim3((unsigned)(gx ? gx : 1), cache->n_layers * 2, batch), dim3(PP_T), 0, reinterpret_cast<cudaStream_t>(stream),
                                   (const uint4*)cache->pages, (uint4*)prefix_kv, cu_prefix_lens, status_word, p, (long long)kv_tokens, (int)chunks));
 }

@@ -298,6 +298,44 @@ def test_keys_that_a_row_does_not_see_have_no_part_in_it(dtype, value, Hq, Hkv, 
     assert torch.isfinite(clean).all()
 
 
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens", [
+    (256, 1, 64, [1, 3], [40, 3]), (128, 1, 128, [2, 1], [200, 130]), (96, 1, 64, [5], [70]), (40, 4, 256, [30, 2], [131, 64]),
+])
+def test_attention_of_wide_groups_of_heads(Hq, Hkv, dh, q_lens, kv_lens):
+    run_attention(Paged(30, q_lens, kv_lens, Hkv, dh, 32), Hq, True)
+
+
+@pytest.mark.parametrize("dtype,q_len", [("bf16", 1), ("bf16", 5), ("f32", 1)])
+def test_attention_of_1024_requests(dtype, q_len):
+    rng = np.random.default_rng(33)
+    kv = [int(x) for x in rng.integers(0, 40, 1024)]
+    q = [min(q_len, n) if i % 7 else 0 for i, n in enumerate(kv)]
+    run_attention(Paged(34, q, kv, 1, 64, 16, dtype), 4, True)
+
+
+@pytest.mark.parametrize("dtype,q_lens,kv_lens", [("bf16", [1, 1, 1], [300, 2, 77]), ("bf16", [40, 9, 1], [300, 9, 77]), ("f32", [3, 1, 1], [300, 2, 77])])
+def test_attention_with_a_table_far_wider_than_the_requests(dtype, q_lens, kv_lens):
+    p = Paged(35, q_lens, kv_lens, 2, 128, 16, dtype)
+    p.table = np.concatenate([p.table, np.full((3, 5000), 2 ** 31 - 1, dtype=np.int32)], axis=1)
+    run_attention(p, 8, True)
+    got, cu = p.cache.pack(ints(p.table), ints(kv_lens), sum(kv_lens) + 100)
+    ref, _ = P.pack(p.pages.view(torch.int16 if dtype == "bf16" else torch.int32).numpy(), kv_lens, p.table, 16)
+    assert np.array_equal(got[:, :, :sum(kv_lens)].contiguous().view(torch.int16 if dtype == "bf16" else torch.int32).cpu().numpy(), ref)
+
+
+def test_attention_writes_nothing_while_the_status_word_is_up():
+    for q_lens, kv_lens, dtype in (([1, 1], [50, 40], "bf16"), ([1], [3000], "bf16"), ([30, 60], [300, 200], "bf16"), ([3, 4], [10, 20], "f32")):
+        p = Paged(36, q_lens, kv_lens, 1, 128, 16, dtype)
+        q = normal(p.rng, (p.T, 4, 128), dtype).cuda()
+        out = torch.full_like(q, 5.0)
+        p.cache.status.fill_(binding.ERR_TIMEOUT)
+        p.cache.attend(1, q, *p.device_args(), out=out)
+        packed, _ = p.cache.pack(ints(p.table), ints(kv_lens), sum(kv_lens), out=torch.full((2, 2, sum(kv_lens), 1, 128), 5.0, dtype=TYPES[dtype], device="cuda"))
+        assert (out == 5.0).all() and (packed == 5.0).all() and p.cache.poll_status() == binding.ERR_TIMEOUT
+        p.cache.attend(1, q, *p.device_args(), out=out)
+        assert p.cache.poll_status() == 0 and not (out == 5.0).any()
+
+
 def test_attention_with_pages_shared_by_requests():
     p = Paged(26, [1, 4, 40], [100, 90, 97], 1, 256, 16)
     p.table[1, :5], p.table[2, :4] = p.table[0, :5], p.table[0, :4]     # a common beginning
@@ -446,6 +484,23 @@ def test_operators_on_a_stream_of_their_own():
     assert torch.equal(want, got) and torch.equal(packed, packed2) and torch.equal(cu, cu2) and torch.equal(qr, q2)
     want = binding.norm_rope_heads(q, k, ints(np.arange(p.T)), rope)
     assert torch.equal(want[0], hq) and torch.equal(want[1], hk)
+
+
+def test_calls_on_two_streams_at_a_time():
+    """Each of them alone fills the device; results as one after the other."""
+    cases = []
+    for seed, Hq, Hkv, dh, q_lens, kv_lens in ((54, 8, 1, 256, [300] * 6, [300] * 6), (55, 8, 2, 128, [200, 77], [3000, 900]), (56, 4, 1, 64, [500, 600], [600, 600]), (57, 8, 1, 256, [1] * 30, [700] * 30)):
+        p = Paged(seed, q_lens, kv_lens, Hkv, dh, 64)
+        q = normal(p.rng, (p.T, Hq, dh)).cuda()
+        args = p.device_args()
+        cases.append((p, q, args, p.cache.attend(1, q, *args).clone()))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(5):
+        got = [p.cache.attend(1, q, *args, stream=st) for (p, q, args, _), st in zip(cases, streams)]
+        torch.cuda.synchronize()
+        for (p, _, _, want), g in zip(cases, got):
+            assert p.cache.poll_status() == 0 and torch.equal(want, g)
 
 
 def test_captured_calls_follow_the_lengths_of_a_replay():

@@ -87,7 +87,8 @@ def test_caches_that_are_refused(lib, cache, status):
 @pytest.mark.parametrize("call", [
     dict(layer=2), dict(hq=0), dict(q=None), dict(q=ADDRESS + 2), dict(q_stride=255), dict(q_stride=260), dict(q_stride=192), dict(batch=0), dict(batch=1025),
     dict(cu=None), dict(lens=None), dict(table=None), dict(most=0), dict(causal=0, prefix=ADDRESS), dict(scale=-1.0), dict(scale=float("nan")),
-    dict(out=None), dict(out=ADDRESS + 4), dict(status=None), dict(most=1 << 28),
+    dict(out=None), dict(out=ADDRESS + 4), dict(status=None), dict(most=1 << 28), dict(cu=ADDRESS + 2), dict(lens=ADDRESS + 1),
+    dict(table=ADDRESS + 3), dict(status=ADDRESS + 2), dict(prefix=ADDRESS + 2), dict(tokens=1 << 31),
 ])
 def test_attention_calls_that_are_refused(lib, call):
     assert _attend(lib, _cache(), **call) == BAD
@@ -104,7 +105,7 @@ def test_attention_heads_that_do_not_divide_are_refused(lib):
     (dict(out_dtype=binding.DTYPES["f32"]), {}, NO), (dict(in_dtype=binding.DTYPES["w4a16"]), {}, NO), ({}, dict(k=None), BAD),
     ({}, dict(q_out=None), BAD), ({}, dict(k_out=None), BAD), ({}, dict(status=None), BAD), ({}, dict(positions=None), BAD),
     ({}, dict(q_stride=128), BAD), ({}, dict(k_stride=32), BAD), ({}, dict(k_stride=68), BAD), ({}, dict(rope=ADDRESS + 4), BAD),
-    ({}, dict(n_positions=0), BAD), ({}, dict(q_gain=ADDRESS + 4), BAD),
+    ({}, dict(n_positions=0), BAD), ({}, dict(q_gain=ADDRESS + 4), BAD), ({}, dict(positions=ADDRESS + 2), BAD), ({}, dict(status=ADDRESS + 1), BAD),
 ])
 def test_head_calls_that_are_refused(lib, desc, call, status):
     a = dict(tokens=3, q=ADDRESS, q_stride=256, k=ADDRESS, k_stride=64, positions=ADDRESS, rope=ADDRESS, n_positions=10, q_gain=None, k_gain=None,
