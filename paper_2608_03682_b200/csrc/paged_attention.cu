@@ -564,10 +564,11 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
     const long long full = (tokens + per - 1) / per > holders ? (tokens + per - 1) / per : holders;
     p.pair = 1, p.units = tokens / per + holders;
     // Key ranges where there are fewer units than one and a half rounds of the pairs, and where the time that splitting saves could be more than
-    // it costs (the kernel cuts the ranges by the lengths, or leaves the units whole: this is the same rule at the longest that they can be).
+    // it costs (the kernel cuts the keys by the lengths, or leaves the units whole: this is the same rule at the longest that they can be).
+    // As many as a unit of three times the average length can have.
     const long long u = full * c->n_kv_heads, tiles = (keys + 127) / 128, rounds = (u + pairs - 1) / pairs;
     long long ranges = 2 * u < 3ll * pairs && tiles * (rounds * pairs - u) > (long long)PAGED_PAIR_MERGE * pairs ? (3ll * pairs + u - 1) / u : 1;
-    if (ranges > keys / 256) ranges = keys / 256;
+    if (ranges > keys / 256 + 1) ranges = keys / 256 + 1;
     p.ranges = (int)(ranges < 1 ? 1 : ranges > 64 ? 64 : ranges);
     return p;
   }

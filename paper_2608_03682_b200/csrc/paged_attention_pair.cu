@@ -30,7 +30,7 @@ namespace {
 
 constexpr int KB = 128;                        // keys per tile: two blocks of 64
 constexpr int PP_THREADS = 20 * 32;
-constexpr int PAIR_LEAST = 2;                  // tiles of keys in a range where units are split, at least
+constexpr int PAIR_LEAST = 2;                  // tiles of keys of a pair where units are split, at least
 
 // head_dim 64: V counts as 128 channels, of which the second CTA's half is zero and never fetched (half of 64 channels would be 64 bytes a
 // key, another operand layout; the products are not what bounds that head_dim).
@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, s_skip;
   __shared__ float xch[2][4][128], xsum[2][4][128];       // what the four threads of a row exchange: maxima (by tile parity), sums (by unit parity)
-  __shared__ int s_first[PAGED_MAX_BATCH + 1], s_warp[PP_THREADS / 32];
+  __shared__ int s_first[PAGED_MAX_BATCH + 1], s_pos[PP_THREADS + 1], s_warp[PP_THREADS / 32];
   __shared__ long long s_sum[PP_THREADS / 32];
   __shared__ int s_most[PP_THREADS / 32];
 
@@ -252,34 +252,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   pdl_wait();
   if (tid == 0) s_skip = status_set(a.status), s_first[0] = 0;
   bool bad = false;
-  int longest = 0x7fffffff;                         // tiles of a key range
-  if (a.ranges > 1) {
-    // such that there are about two ranges for each pair, and not many more (a unit's last range is half as long on average)
-    long long tiles = 0;
-    int units = 0, most = 0;
-    for (int i = tid; i < a.pb.batch; i += PP_THREADS) {
-      const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1], kv = a.pb.kv_lens[i];
-      if (paged_entry_bad(a.pb, i, lo, hi, kv, false)) continue;
-      const int n = (hi - lo + 2 * TOK - 1) / (2 * TOK);
-      units += n, tiles += (long long)n * ((kv + KB - 1) / KB);
-      if (n) most = max(most, (kv + KB - 1) / KB);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, o), units += __shfl_xor_sync(0xffffffffu, units, o);
-    most = __reduce_max_sync(0xffffffffu, most);
-    if (lane == 0) s_sum[warp] = tiles, s_warp[warp] = units, s_most[warp] = most;
-    __syncthreads();
-    tiles = 0, units = 0;
-    for (int w = 0; w < PP_THREADS / 32; ++w) tiles += s_sum[w], units += s_warp[w], most = max(most, s_most[w]);
-    __syncthreads();
-    const long long pieces = 2ll * n_pairs - (long long)units * a.hkv / 2, per = pieces > 0 ? (tiles * a.hkv + pieces - 1) / pieces : 0x7fffffff;
-    longest = (int)(per < PAIR_LEAST ? PAIR_LEAST : per > 0x7fffffff ? 0x7fffffff : per);
-    // (fp32 results and the second kernel cost what PAGED_PAIR_MERGE tiles do: not where the longest units, left whole, end before that)
-    const long long whole = (long long)most * (((long long)units * a.hkv + n_pairs - 1) / n_pairs);
-    if (whole <= tiles * a.hkv / n_pairs + PAGED_PAIR_MERGE) longest = 0x7fffffff;
-  }
-  auto ranges_for = [&](int kv) { return a.ranges > 1 ? min(a.ranges, max(1, ((kv + KB - 1) / KB - 1) / longest + 1)) : 1; };
-  int acc = 0;                                      // key ranges of units (of one kv head) so far
+  int acc = 0;                                      // units (of one kv head) so far
   for (int i0 = 0; i0 < a.pb.batch; i0 += PP_THREADS) {
     const int i = i0 + tid;
     int n = 0;
@@ -287,7 +260,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
       const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1], kv = a.pb.kv_lens[i];
       const bool b = paged_entry_bad(a.pb, i, lo, hi, kv, false);
       bad |= b;
-      n = b ? 0 : (hi - lo + 2 * TOK - 1) / (2 * TOK) * ranges_for(kv);
+      n = b ? 0 : (hi - lo + 2 * TOK - 1) / (2 * TOK);
     }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -309,12 +282,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   const bool skip = s_skip != 0;
   const int n_units = bad ? 0 : acc * a.hkv;
 
-  // Units of this pair: of every round of n_pairs units one, rounds dealt back and forth (a request's last, longest tiles come first).
-  auto index_of = [&](int k) { return k * n_pairs + ((k & 1) ? n_pairs - 1 - pair : pair); };
-  auto unit_at = [&](int j) {
+  auto unit_at = [&](int ut) {                      // without a kv head
     Unit u;
-    const int ut = a.hkv > 1 ? j / a.hkv : j;
-    u.hk = j - ut * a.hkv, u.pad = 0;
+    u.hk = u.pad = 0;
     int lo = 0, hi = a.pb.batch;                    // s_first[lo] <= ut < s_first[hi]
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -323,21 +293,72 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     }
     u.r.b = lo, u.r.lo = a.pb.cu[lo], u.r.n = a.pb.cu[lo + 1] - u.r.lo, u.r.kv = a.pb.kv_lens[lo];
     u.r.prefix = a.prefix_lens ? min(max(a.prefix_lens[lo], 0), u.r.kv) : 0;
-    const int ranges = ranges_for(u.r.kv), from_end = s_first[lo + 1] - 1 - ut, ui = from_end / ranges;
-    u.tok0 = ui * 2 * TOK, u.range = from_end - ui * ranges;
-    const int keys = u.r.limit(min(u.tok0 + 2 * TOK, u.r.n) - 1, a.causal), tiles = max(1, (keys + KB - 1) / KB);
-    u.ranges = min(ranges, tiles);                  // (none of them empty)
-    u.t0 = u.range < u.ranges ? (int)((long long)tiles * u.range / u.ranges) : 0;
-    u.T = u.range < u.ranges ? (int)((long long)tiles * (u.range + 1) / u.ranges) - u.t0 : 0;
+    u.tok0 = (s_first[lo + 1] - 1 - ut) * 2 * TOK;  // (a request's last, longest unit comes first)
+    const int keys = u.r.limit(min(u.tok0 + 2 * TOK, u.r.n) - 1, a.causal);
+    u.t0 = 0, u.T = max(1, (keys + KB - 1) / KB), u.range = 0, u.ranges = 1;
     return u;
   };
-  // the first unit of this pair from its round k on; k moves past it
-  auto next_unit = [&](int& k) {
-    for (int j; (j = index_of(k)) < n_units || k * n_pairs < n_units;) {
-      ++k;
-      if (j >= n_units) continue;
-      const Unit u = unit_at(j);
-      if (u.T > 0) return u;
+
+  // ---- Few units: all their tiles in a row, an equal part of it for each pair, so that a pair ends one unit and begins another.  `each`: tiles
+  // of a pair (0: the units stay whole).  s_pos: tiles before each unit, of one kv head.  A unit of T tiles meets (T - 2) / each + 2 pairs at
+  // most: no more than the workspace has room for.
+  int each = 0;
+  if (a.ranges > 1 && !bad && acc <= PP_THREADS) {
+    const int mine = tid < acc ? unit_at(tid).T : 0;
+    long long upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long up = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += up;
+    }
+    int most = __reduce_max_sync(0xffffffffu, mine);
+    if (lane == 31) s_sum[warp] = upto, s_most[warp] = most;
+    __syncthreads();
+    long long tiles = 0;
+    for (int w = 0; w < PP_THREADS / 32; ++w) {
+      if (w < warp) upto += s_sum[w];
+      tiles += s_sum[w], most = max(most, s_most[w]);
+    }
+    s_pos[tid + 1] = (int)upto;
+    if (tid == 0) s_pos[0] = 0;
+    __syncthreads();
+    tiles *= a.hkv;
+    // (fp32 results and the second kernel cost what PAGED_PAIR_MERGE tiles do: not where the longest units, left whole, end before that)
+    const long long per = (tiles + n_pairs - 1) / n_pairs, whole = (long long)most * ((n_units + n_pairs - 1) / n_pairs);
+    if (whole > per + PAGED_PAIR_MERGE && tiles <= 0x7fffffffll) each = max(max(PAIR_LEAST, (int)per), (most - 1) / (a.ranges - 1) + 1);
+  }
+  // Units of this pair, `at` of the first: 0, or the first of its tiles.  Whole ones: of every round of n_pairs units one, rounds dealt back
+  // and forth.
+  const int begin = each ? (int)min((long long)pair * each, 0x7fffffffll) : 0;
+  auto next_unit = [&](int& at) {                   // the first one from `at` on; moves past it
+    if (each) {
+      const int total = s_pos[acc] * a.hkv, end = (int)min((long long)begin + each, (long long)total);
+      if (at < end) {
+        int lo = 0, hi = acc;                       // s_pos[lo] * hkv <= at < s_pos[hi] * hkv
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (s_pos[mid] * a.hkv <= at) lo = mid;
+          else hi = mid;
+        }
+        Unit u = unit_at(lo);
+        const int first = s_pos[lo] * a.hkv;
+        u.hk = (at - first) / u.T;
+        const int start = first + u.hk * u.T, stop = start + u.T;
+        u.range = pair - start / each, u.ranges = (stop - 1) / each - start / each + 1;
+        u.t0 = at - start, u.T = min(stop, end) - at;
+        at = min(stop, end);
+        return u;
+      }
+    } else {
+      for (int j; at * n_pairs < n_units;) {
+        j = at * n_pairs + ((at & 1) ? n_pairs - 1 - pair : pair);
+        ++at;
+        if (j >= n_units) continue;
+        const int ut = a.hkv > 1 ? j / a.hkv : j;
+        Unit u = unit_at(ut);
+        u.hk = j - ut * a.hkv;
+        return u;
+      }
     }
     Unit u{};
     u.r.b = -1, u.T = 0;
@@ -395,7 +416,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     __syncwarp();
   } else if (warp == 2) {
     // =========================== the pair's units ============================================================================
-    int k = 0;
+    int k = begin;
     for (int i = 0;; ++i) {
       const Unit u = next_unit(k);
       if (i >= UNITS) wait_warp(smem_u32(&u_free[i % UNITS]), (uint32_t)(i / UNITS - 1) & 1u, wl);
@@ -616,7 +637,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
       rows_sync(q);                           // (maxima beside a range's result: written by another warp of the quarter)
     }
     if (a.causal && __any_sync(0xffffffffu, odd) && !*reinterpret_cast<volatile int*>(&abort_flag)) {
-      int k = 0;
+      int k = begin;
       for (Unit u = next_unit(k); u.r.b >= 0; u = next_unit(k)) {
         const int n_rows = min(TOK, u.r.n - u.tok0 - half * TOK) * G, end = min((u.t0 + u.T) * KB, u.r.kv);
         for (int rr = q * 32; rr < min(n_rows, q * 32 + 32); ++rr) {
