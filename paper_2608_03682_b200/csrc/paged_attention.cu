@@ -492,8 +492,22 @@ __global__ void __launch_bounds__(128) k_paged_merge(const PagedAttn a) {
   const int tok = (int)(row / a.hq);
   // (the lengths and the word say whether there is anything in the workspace; its entries are on their way meanwhile)
   const bool live = !status_set(a.status) && tok >= a.pb.cu[0] && tok < a.pb.cu[a.pb.batch];
-  const int most = a.ranges;
-  float4 ml = lane < most ? a.part_ml[(size_t)lane * rows + row] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  float4 ml = lane < a.ranges ? a.part_ml[(size_t)lane * rows + row] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  const float* p = a.part_o + (size_t)row * DH + c;
+  float x[4][C];
+  auto load = [&](float (&to)[C], int k) {
+#pragma unroll
+    for (int e = 0; e < C; e += V) {
+      if constexpr (V == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p + (size_t)k * rows * DH + e);
+        to[e] = v.x, to[e + 1] = v.y, to[e + 2] = v.z, to[e + 3] = v.w;
+      } else {
+        const float2 v = *reinterpret_cast<const float2*>(p + (size_t)k * rows * DH + e);
+        to[e] = v.x, to[e + 1] = v.y;
+      }
+    }
+  };
+  load(x[0], 0), load(x[1], 1);                             // (where a row has ranges it has two; a.ranges > 1: there is memory to read)
   if (!live) return;
   const int ranges = (int)__shfl_sync(0xffffffffu, ml.z, 0);
   if (ranges <= 1) return;
@@ -504,24 +518,15 @@ __global__ void __launch_bounds__(128) k_paged_merge(const PagedAttn a) {
   const float w1 = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M), w2 = ml2.x == -INFINITY ? 0.f : exp2f(ml2.x - M);
   const float sum = warp_sum(w1 * ml.y + w2 * ml2.y);
   float o[C] = {};
-  const float* p = a.part_o + (size_t)row * DH + c;
   for (int k0 = 0; k0 < ranges; k0 += 4) {
-    float x[4][C];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 4; ++j) {
+      if (k0 + j < ranges && (k0 > 0 || j >= 2)) load(x[j], k0 + j);
+      if (k0 + j >= ranges) {
 #pragma unroll
-      for (int e = 0; e < C; e += V) {
-        if (k0 + j >= ranges) {
-#pragma unroll
-          for (int v = 0; v < V; ++v) x[j][e + v] = 0.f;
-        } else if constexpr (V == 4) {
-          const float4 v = *reinterpret_cast<const float4*>(p + (size_t)(k0 + j) * rows * DH + e);
-          x[j][e] = v.x, x[j][e + 1] = v.y, x[j][e + 2] = v.z, x[j][e + 3] = v.w;
-        } else {
-          const float2 v = *reinterpret_cast<const float2*>(p + (size_t)(k0 + j) * rows * DH + e);
-          x[j][e] = v.x, x[j][e + 1] = v.y;
-        }
+        for (int e = 0; e < C; ++e) x[j][e] = 0.f;
       }
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float w = __shfl_sync(0xffffffffu, k0 + j < 32 ? w1 : w2, (k0 + j) & 31);      // (0 past the ranges)
