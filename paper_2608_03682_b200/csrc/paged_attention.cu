@@ -597,7 +597,7 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
   return p;
 }
 size_t partial_bytes(const Plan& p, int hq, int dh, int tokens) {
-  return p.ranges > 1 ? (size_t)p.ranges * tokens * hq * ((size_t)dh * 4 + 16) : 0;
+  return p.ranges > 1 ? (size_t)p.ranges * tokens * hq * ((size_t)dh * 4 + 16) + 16 : 0;      // (16: the accumulators begin on 32 bytes)
 }
 
 template <typename K>
@@ -692,7 +692,7 @@ phyai_status_t phyai_paged_attention(const phyai_paged_cache_t* cache, uint32_t 
   a.prefix_lens = prefix_lens, a.causal = causal ? 1 : 0, a.hq = (int)n_q_heads, a.hkv = (int)cache->n_kv_heads, a.group = a.hq / a.hkv;
   a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)dh)) * LOG2E;
   a.ranges = p.ranges, a.status = status_word, a.wait_limit = 1u << 22;
-  a.part_ml = reinterpret_cast<float4*>(workspace), a.part_o = reinterpret_cast<float*>(a.part_ml + (size_t)p.ranges * tokens * n_q_heads);
+  a.part_ml = reinterpret_cast<float4*>(workspace), a.part_o = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(a.part_ml + (size_t)p.ranges * tokens * n_q_heads) + 31) & ~(uintptr_t)31);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaErrorInvalidValue;
   if (p.f32) {

@@ -115,6 +115,8 @@ struct Ring {
   }
 };
 
+// the two loading warps: the first keys and queries go ahead of the first values
+__device__ __forceinline__ void first_copies() { asm volatile("bar.sync 1, 64;" ::: "memory"); }
 // the four warps that share the rows of a tensor-memory lane quarter
 __device__ __forceinline__ void rows_sync(int q) { asm volatile("bar.sync %0, 128;" ::"r"(4 + q) : "memory"); }
 
@@ -193,6 +195,7 @@ struct alignas(16) Unit {
   int range, ranges;
   int pad;
 };
+constexpr int SPLIT_UNITS = 640;               // units of a kv head, at most, where they are split (the launch asks for it with one and a half a pair at most)
 constexpr int UNITS = 8;                       // units that the scheduling warp is ahead, at most
 
 template <int DH>
@@ -211,9 +214,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, s_skip;
   __shared__ float xch[2][4][128], xsum[2][4][128];       // what the four threads of a row exchange: maxima (by tile parity), sums (by unit parity)
-  __shared__ int s_first[PAGED_MAX_BATCH + 1], s_pos[PP_THREADS + 1], s_warp[PP_THREADS / 32];
-  __shared__ long long s_sum[PP_THREADS / 32];
-  __shared__ int s_most[PP_THREADS / 32];
+  __shared__ int s_first[PAGED_MAX_BATCH + 1], s_pos[SPLIT_UNITS + 1], s_list[3];
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int half = blockIdx.x & 1, pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
@@ -248,40 +249,22 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
   const uint32_t tmem_s = tmem_base, tmem_o = tmem_base + NB * KB;
   const WaitCtx wc{a.status, &abort_flag, a.wait_limit, true}, wl = wc;
 
-  // ---- units before each request (both CTAs of a pair read the same lengths and come to the same list)
+  // ---- units of each request (both CTAs of a pair read the same lengths and come to the same list)
   pdl_wait();
   if (tid == 0) s_skip = status_set(a.status), s_first[0] = 0;
   bool bad = false;
-  int acc = 0;                                      // units (of one kv head) so far
-  for (int i0 = 0; i0 < a.pb.batch; i0 += PP_THREADS) {
-    const int i = i0 + tid;
-    int n = 0;
-    if (i < a.pb.batch) {
-      const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1], kv = a.pb.kv_lens[i];
-      const bool b = paged_entry_bad(a.pb, i, lo, hi, kv, false);
-      bad |= b;
-      n = b ? 0 : (hi - lo + 2 * TOK - 1) / (2 * TOK);
-    }
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, n, o);
-      if (lane >= o) n += up;
-    }
-    if (lane == 31) s_warp[warp] = n;
-    __syncthreads();
-    int before = acc;
-    for (int w = 0; w < PP_THREADS / 32; ++w) {
-      if (w < warp) before += s_warp[w];
-      acc += s_warp[w];
-    }
-    if (i < a.pb.batch) s_first[i + 1] = before + n;
-    __syncthreads();
+  for (int i = tid; i < a.pb.batch; i += PP_THREADS) {
+    const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1], kv = a.pb.kv_lens[i];
+    const bool b = paged_entry_bad(a.pb, i, lo, hi, kv, false);
+    bad |= b;
+    s_first[i + 1] = b ? 0 : (hi - lo + 2 * TOK - 1) / (2 * TOK);
   }
   bad = __syncthreads_or(bad);
   if (bad && tid == 0) atomicExch(a.status, ST_INVALID_ARG);
   const bool skip = s_skip != 0;
-  const int n_units = bad ? 0 : acc * a.hkv;
 
+  // ---- what warp 2 goes by (and, once it has published its last unit, others): s_first: units (of one kv head) before each request; units of one kv
+  // head; `each`: 0, or the tiles of a pair where units are split; s_pos: tiles before each unit, of one kv head.
   auto unit_at = [&](int ut) {                      // without a kv head
     Unit u;
     u.hk = u.pad = 0;
@@ -298,70 +281,46 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     u.t0 = 0, u.T = max(1, (keys + KB - 1) / KB), u.range = 0, u.ranges = 1;
     return u;
   };
-
-  // ---- Few units: all their tiles in a row, an equal part of it for each pair, so that a pair ends one unit and begins another.  `each`: tiles
-  // of a pair (0: the units stay whole).  s_pos: tiles before each unit, of one kv head.  A unit of T tiles meets (T - 2) / each + 2 pairs at
-  // most: no more than the workspace has room for.
-  int each = 0;
-  if (a.ranges > 1 && !bad && acc <= PP_THREADS) {
-    const int mine = tid < acc ? unit_at(tid).T : 0;
-    long long upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long up = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += up;
-    }
-    int most = __reduce_max_sync(0xffffffffu, mine);
-    if (lane == 31) s_sum[warp] = upto, s_most[warp] = most;
-    __syncthreads();
-    long long tiles = 0;
-    for (int w = 0; w < PP_THREADS / 32; ++w) {
-      if (w < warp) upto += s_sum[w];
-      tiles += s_sum[w], most = max(most, s_most[w]);
-    }
-    s_pos[tid + 1] = (int)upto;
-    if (tid == 0) s_pos[0] = 0;
-    __syncthreads();
-    tiles *= a.hkv;
-    // (fp32 results and the second kernel cost what PAGED_PAIR_MERGE tiles do: not where the longest units, left whole, end before that)
-    const long long per = (tiles + n_pairs - 1) / n_pairs, whole = (long long)most * ((n_units + n_pairs - 1) / n_pairs);
-    if (whole > per + PAGED_PAIR_MERGE && tiles <= 0x7fffffffll) each = max(max(PAIR_LEAST, (int)per), (most - 1) / (a.ranges - 1) + 1);
-  }
-  // Units of this pair, `at` of the first: 0, or the first of its tiles.  Whole ones: of every round of n_pairs units one, rounds dealt back
-  // and forth.
-  const int begin = each ? (int)min((long long)pair * each, 0x7fffffffll) : 0;
-  auto next_unit = [&](int& at) {                   // the first one from `at` on; moves past it
+  // The pair's first unit from `at` on, which moves past it.  Whole units: of every round of n_pairs units one, rounds dealt back and forth;
+  // `at` counts rounds.  Split ones: all their tiles in a row, an equal part of it for each pair, so that a pair ends one unit and begins another;
+  // `at` is a tile.  A unit of T tiles meets (T - 2) / each + 2 pairs at most: no more than the workspace has room for.
+  auto next_unit = [&](int& at, int units, int each) {
+    int ut, hk = 0, start = at;
+    bool any;
     if (each) {
-      const int total = s_pos[acc] * a.hkv, end = (int)min((long long)begin + each, (long long)total);
-      if (at < end) {
-        int lo = 0, hi = acc;                       // s_pos[lo] * hkv <= at < s_pos[hi] * hkv
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (s_pos[mid] * a.hkv <= at) lo = mid;
-          else hi = mid;
-        }
-        Unit u = unit_at(lo);
-        const int first = s_pos[lo] * a.hkv;
-        u.hk = (at - first) / u.T;
-        const int start = first + u.hk * u.T, stop = start + u.T;
-        u.range = pair - start / each, u.ranges = (stop - 1) / each - start / each + 1;
-        u.t0 = at - start, u.T = min(stop, end) - at;
-        at = min(stop, end);
-        return u;
+      const int total = s_pos[units] * a.hkv;
+      any = at < (int)min((long long)(pair + 1) * each, (long long)total);
+      int lo = 0, hi = units;                       // s_pos[lo] * hkv <= at < s_pos[hi] * hkv
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s_pos[mid] * a.hkv <= at) lo = mid;
+        else hi = mid;
       }
+      ut = lo;
     } else {
-      for (int j; at * n_pairs < n_units;) {
-        j = at * n_pairs + ((at & 1) ? n_pairs - 1 - pair : pair);
-        ++at;
-        if (j >= n_units) continue;
-        const int ut = a.hkv > 1 ? j / a.hkv : j;
-        Unit u = unit_at(ut);
-        u.hk = j - ut * a.hkv;
-        return u;
+      for (;; ++at) {
+        ut = at * n_pairs + ((at & 1) ? n_pairs - 1 - pair : pair), any = at * n_pairs < units * a.hkv;
+        if (!any || ut < units * a.hkv) break;
       }
+      ++at;
+      if (a.hkv > 1) hk = ut % a.hkv, ut /= a.hkv;
     }
-    Unit u{};
-    u.r.b = -1, u.T = 0;
+    if (!any) {
+      Unit u{};
+      u.r.b = -1, u.T = 0;
+      return u;
+    }
+    Unit u = unit_at(ut);
+    u.hk = hk;
+    if (each) {
+      start = s_pos[ut] * a.hkv;
+      if (a.hkv > 1) u.hk = (at - start) / u.T, start += u.hk * u.T;
+      const int first = start / each, stop = start + u.T;
+      u.range = pair - first, u.ranges = (stop - 1) / each - first + 1;
+      u.t0 = at - start;
+      at = (int)min((long long)stop, (long long)(pair + 1) * each);
+      u.T = at - start - u.t0;
+    }
     return u;
   };
   // The units come through shared memory from a warp of their own: some 400 instructions each (searches, divisions), which every warp
@@ -410,15 +369,56 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
           __syncwarp();
           if (lane < DH / 64)
             copy4d(Qs + (uint32_t)lane * (128 * 128), &tmq, u.hk * G, u.r.lo + u.tok0 + half * TOK, lane, smem_u32(&q_full) & LEADER_MASK);
+          if (n == 0) first_copies();
         }
       }
     }
     __syncwarp();
   } else if (warp == 2) {
     // =========================== the pair's units ============================================================================
-    int k = begin;
+    int units = 0, each = 0, at = 0;
+    if (!bad) {
+      for (int i0 = 0; i0 < a.pb.batch; i0 += 32) {
+        int n = i0 + lane < a.pb.batch ? s_first[i0 + lane + 1] : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int up = __shfl_up_sync(0xffffffffu, n, o);
+          if (lane >= o) n += up;
+        }
+        if (i0 + lane < a.pb.batch) s_first[i0 + lane + 1] = units + n;
+        units += __shfl_sync(0xffffffffu, n, 31);
+      }
+      __syncwarp();
+    }
+    if (a.ranges > 1 && units > 0 && units <= SPLIT_UNITS) {
+      long long tiles = 0;
+      int most = 0;
+      for (int i0 = 0; i0 < units; i0 += 32) {
+        const int T = i0 + lane < units ? unit_at(i0 + lane).T : 0;
+        int n = T;                                  // (32 x 2^24 at most)
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int up = __shfl_up_sync(0xffffffffu, n, o);
+          if (lane >= o) n += up;
+        }
+        if (i0 + lane < units) s_pos[i0 + lane + 1] = (int)tiles + n;
+        tiles += __shfl_sync(0xffffffffu, n, 31), most = max(most, T);
+      }
+      if (lane == 0) s_pos[0] = 0;
+      __syncwarp();
+      most = __reduce_max_sync(0xffffffffu, most);
+      tiles *= a.hkv;
+      // (fp32 results and the second kernel cost what PAGED_PAIR_MERGE tiles do: not where the longest units, left whole, end before that)
+      if (tiles <= 0x7fffffff - n_pairs) {
+        const int per = ((int)tiles + n_pairs - 1) / n_pairs;
+        const long long whole = (long long)most * ((units * a.hkv + n_pairs - 1) / n_pairs);
+        if (whole > per + PAGED_PAIR_MERGE) each = max(max(PAIR_LEAST, per), (most - 1) / (a.ranges - 1) + 1);
+      }
+    }
+    if (each) at = (int)min((long long)pair * each, 0x7fffffffll);
+    if (lane == 0) s_list[0] = units, s_list[1] = each, s_list[2] = at;
     for (int i = 0;; ++i) {
-      const Unit u = next_unit(k);
+      const Unit u = next_unit(at, units, each);
       if (i >= UNITS) wait_warp(smem_u32(&u_free[i % UNITS]), (uint32_t)(i / UNITS - 1) & 1u, wl);
       if (lane == 0) {
         s_unit[i % UNITS] = u;
@@ -451,6 +451,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
           else remote_arrive(full_lead + (uint32_t)bf * 8u);
         }
         __syncwarp();
+        if (n == 0) first_copies();
         bar = clear ? smem_u32(&v_own) : bar & LEADER_MASK;
         if (fetch && lane < 2 * nb)
           copy4d(dst + (uint32_t)blk * L::PIECE + (uint32_t)ch * L::KBLOCK + (uint32_t)pc * piece_bytes, &tmkv, row, u.hk * (DH / 64) + half * (DH / 128) + ch,
@@ -600,7 +601,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
           if (row < n_rows) {
             float* p = a.part_o + slot * DH + c0 + c;
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            for (int e = 0; e < 16; e += 8)        // (whole sectors)
+              asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p + e), "f"(o[e]), "f"(o[e + 1]), "f"(o[e + 2]), "f"(o[e + 3]), "f"(o[e + 4]),
+                           "f"(o[e + 5]), "f"(o[e + 6]), "f"(o[e + 7])
+                           : "memory");
           }
 #pragma unroll
           for (int e = 0; e < 16; ++e) fin = fmaf(o[e], 0.f, fin);
@@ -637,8 +641,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
       rows_sync(q);                           // (maxima beside a range's result: written by another warp of the quarter)
     }
     if (a.causal && __any_sync(0xffffffffu, odd) && !*reinterpret_cast<volatile int*>(&abort_flag)) {
-      int k = begin;
-      for (Unit u = next_unit(k); u.r.b >= 0; u = next_unit(k)) {
+      int at = s_list[2];
+      for (Unit u = next_unit(at, s_list[0], s_list[1]); u.r.b >= 0; u = next_unit(at, s_list[0], s_list[1])) {
         const int n_rows = min(TOK, u.r.n - u.tok0 - half * TOK) * G, end = min((u.t0 + u.T) * KB, u.r.kv);
         for (int rr = q * 32; rr < min(n_rows, q * 32 + 32); ++rr) {
           const int rt = rr / G, tok = u.r.lo + u.tok0 + half * TOK + rt, head = u.hk * G + rr - rt * G;
