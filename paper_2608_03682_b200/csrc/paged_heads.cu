@@ -5,9 +5,13 @@
 //
 // A head x of dh channels becomes  y = x * rsqrt(mean(x^2) + eps) * (1 + gain)  and then, for j < dh / 2,
 //   (y_j, y_{j + dh/2}) -> (y_j cos - y_{j + dh/2} sin, y_{j + dh/2} cos + y_j sin)  with the table's row of its position.
-// Everything is read once and written once, so memory bounds it: a lane takes 16 bytes of a head's
-// channels and their rotary partners, so that only the sum of squares crosses lanes (with 8 channels a lane and the
-// partners by shuffles, shuffles and table loads bounded it).  The arithmetic is fp32 with one rounding at the store.
+// Everything is read once and written once, so memory bounds it: a lane takes 16 bytes of a head's channels and their rotary partners, so
+// that only the sum of squares crosses lanes (with 8 channels a lane and the partners by shuffles, shuffles and table loads bounded it).  The
+// channels are pairs, a warp's next to one another: a pair's table entry is 16 bytes, so that a load of the table or the gains takes as few passes of
+// the L1 as it can (with 8 channels in a row, one load of 16 bytes, a lane's entries are 64 bytes apart: 17.1 for 15.0 us).  The arithmetic is
+// fp32 with one rounding at the store.
+// Measured: 7744 tokens of 9 heads of 256 (pi0), bf16: 15.0 us, 4.8 TB/s; with the append (k, v into pages) 14.5.  64 tokens: 2 - 3 us, the
+// chain lengths -> page -> table -> store.  Packing 258 MB: 38.9 us, 6.0 TB/s of 6.55 that a copy reaches.
 #include <cstdio>
 
 #include "../../include/phyai.h"
@@ -19,42 +23,41 @@ thread_local char g_paged_err[256] = "";
 
 namespace {
 
-// 16 bytes of consecutive channels, as stored
+// A lane's channels of half a head, as stored: 16 bytes, in pairs `apart` channels from one another.
 template <typename T>
 struct Raw;
 template <>
 struct Raw<float> {
   static constexpr int N = 4;
-  float4 a;
-  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); }
-  __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w; }
+  float2 a[2];
+  __device__ __forceinline__ void load(const float* p, int apart) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) a[j] = *reinterpret_cast<const float2*>(p + j * apart);
+  }
+  __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = a[0].x, v[1] = a[0].y, v[2] = a[1].x, v[3] = a[1].y; }
 };
 template <>
 struct Raw<__nv_bfloat16> {
   static constexpr int N = 8;
-  uint4 a;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+  uint32_t a[4];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int apart) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(u[i] << 16), v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    for (int j = 0; j < 4; ++j) a[j] = *reinterpret_cast<const uint32_t*>(p + j * apart);
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(a[i] << 16), v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
   }
 };
 template <int N>
-__device__ __forceinline__ void store_channels(float* p, const float (&x)[N]) {
+__device__ __forceinline__ void store_channels(float* p, const float (&x)[N], int apart) {
 #pragma unroll
-  for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+  for (int i = 0; i < N; i += 2) *reinterpret_cast<float2*>(p + i / 2 * apart) = make_float2(x[i], x[i + 1]);
 }
 template <int N>
-__device__ __forceinline__ void store_channels(__nv_bfloat16* p, const float (&x)[N]) {
-  uint32_t u[N / 2];
+__device__ __forceinline__ void store_channels(__nv_bfloat16* p, const float (&x)[N], int apart) {
 #pragma unroll
-  for (int i = 0; i < N / 2; ++i) {
-    const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    u[i] = *reinterpret_cast<const uint32_t*>(&b);
-  }
-  if constexpr (N == 8) *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
-  else *reinterpret_cast<uint2*>(p) = make_uint2(u[0], u[1]);
+  for (int i = 0; i < N; i += 2) *reinterpret_cast<__nv_bfloat162*>(p + i / 2 * apart) = __floats2bfloat162_rn(x[i], x[i + 1]);
 }
 
 struct HeadsArgs {
@@ -72,16 +75,17 @@ struct HeadsArgs {
   int* status;
 };
 
-constexpr int HT = 256, HB = 3;          // threads of a block, blocks of an SM
+constexpr int HT = 256, HB = 4;          // threads of a block, blocks of an SM
 
-// A lane takes 16 bytes of channels (C of them) and their rotary partners of a head, a warp 64 C / dh heads of a token at a time (a slot);
-// slots run over the tokens, a warp takes U in a row and issues all their loads before it uses the first.
+// A lane takes C channels and their rotary partners of a head, a warp 64 C / dh heads of a token at a time (a slot); slots run over the tokens, a
+// warp takes U in a row and issues all their loads before it uses the first.  Two slots and four blocks: 15.0 us for the above; one slot 15.0 (append
+// 14.8 for 14.5), three 18.8, three blocks 15.7, five 17 and more (spills); the loads of the next slots under these: 18.7 (registers).
 template <int DH, typename IN, typename OUT, bool APPEND, int U>
 __global__ void __launch_bounds__(HT, HB) k_heads(const HeadsArgs a) {
-  constexpr int C = Raw<IN>::N, HALF = DH / 2, LANES = HALF / C, HPS = 32 / LANES;           // lanes per head, heads per slot
+  constexpr int C = Raw<IN>::N, HALF = DH / 2, LANES = HALF / C, HPS = 32 / LANES, APART = LANES * 2;           // lanes per head, heads per slot
   __shared__ int s_cu[APPEND ? PAGED_MAX_BATCH + 1 : 1], s_kv[APPEND ? PAGED_MAX_BATCH : 1];
   __shared__ int s_skip;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LANES, c = (lane % LANES) * C;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LANES, c = (lane % LANES) * 2;
   const int hq = a.q ? a.hq : 0, H = hq + a.hkv + (a.v ? a.hkv : 0), slots = (H + HPS - 1) / HPS;
   const int step = (int)gridDim.x * (HT / 32) * U, step_tok = step / slots, step_slot = step - step_tok * slots;
   pdl_launch_dependents();
@@ -116,7 +120,7 @@ __global__ void __launch_bounds__(HT, HB) k_heads(const HeadsArgs a) {
         if (h < H && tok < a.tokens) {
           const IN* p = h < hq ? (const IN*)a.q + tok * a.q_stride + h * DH
                                : h < hq + a.hkv ? (const IN*)a.k + tok * a.k_stride + (h - hq) * DH : (const IN*)a.v + tok * a.v_stride + (h - hq - a.hkv) * DH;
-          lo[u].load(p + c), hi[u].load(p + c + HALF);
+          lo[u].load(p + c, APART), hi[u].load(p + c + HALF, APART);
         } else {
           lo[u] = hi[u] = Raw<IN>{};
         }
@@ -154,11 +158,11 @@ __global__ void __launch_bounds__(HT, HB) k_heads(const HeadsArgs a) {
           }
         }
         if (ok && a.rope) {
-          const float4* t = reinterpret_cast<const float4*>(a.rope + ((size_t)pos * HALF + c) * 2);
+          const float* t = a.rope + ((size_t)pos * HALF + c) * 2;
 #pragma unroll
-          for (int i = 0; i < C / 2; ++i) {
-            const float4 w = __ldg(t + i);
-            cs[2 * i] = w.x, sn[2 * i] = w.y, cs[2 * i + 1] = w.z, sn[2 * i + 1] = w.w;
+          for (int i = 0; i < C; i += 2) {
+            const float4 w = __ldg(reinterpret_cast<const float4*>(t + i * APART));
+            cs[i] = w.x, sn[i] = w.y, cs[i + 1] = w.z, sn[i + 1] = w.w;
           }
         }
       }
@@ -174,10 +178,11 @@ __global__ void __launch_bounds__(HT, HB) k_heads(const HeadsArgs a) {
       if (gain) {
         const float r = rsqrtf(ss * (1.0f / DH) + a.eps);
 #pragma unroll
-        for (int i = 0; i < C; i += 4) {
-          const float4 g = __ldg(reinterpret_cast<const float4*>(gain + c + i)), f = __ldg(reinterpret_cast<const float4*>(gain + c + HALF + i));
-          x[i] *= fmaf(r, g.x, r), x[i + 1] *= fmaf(r, g.y, r), x[i + 2] *= fmaf(r, g.z, r), x[i + 3] *= fmaf(r, g.w, r);
-          y[i] *= fmaf(r, f.x, r), y[i + 1] *= fmaf(r, f.y, r), y[i + 2] *= fmaf(r, f.z, r), y[i + 3] *= fmaf(r, f.w, r);
+        for (int i = 0; i < C; i += 2) {
+          const float* at = gain + c + i / 2 * APART;
+          const float2 g = __ldg(reinterpret_cast<const float2*>(at)), f = __ldg(reinterpret_cast<const float2*>(at + HALF));
+          x[i] *= fmaf(r, g.x, r), x[i + 1] *= fmaf(r, g.y, r);
+          y[i] *= fmaf(r, f.x, r), y[i + 1] *= fmaf(r, f.y, r);
         }
       }
       if (a.rope && kind < 2) {
@@ -192,7 +197,7 @@ __global__ void __launch_bounds__(HT, HB) k_heads(const HeadsArgs a) {
         OUT* p = kind == 0 ? (OUT*)a.q_out + ((size_t)tok * a.hq + h) * DH
                  : APPEND  ? (OUT*)(kind == 1 ? a.k_plane : a.v_plane) + ((size_t)row * a.hkv + (kind == 1 ? h - hq : h - hq - a.hkv)) * DH
                            : (OUT*)a.k_out + ((size_t)tok * a.hkv + h - hq) * DH;
-        store_channels(p + c, x), store_channels(p + c + HALF, y);
+        store_channels(p + c, x, APART), store_channels(p + c + HALF, y, APART);
       }
       if (++slot == slots) slot = 0, ++tok;
     }
