@@ -13,7 +13,10 @@
 //   O^T += V^T P^T   V^T by transposing ldmatrix
 // The warps of a block merge through shared memory, the blocks of a cluster through distributed shared memory, several clusters of a
 // row (key ranges) through a second kernel.
+// Measured, one token a request: 8 heads of 256, 64 requests of 601 - 969 keys 12.5 us, 4.1 TB/s, 256 41 us, 5.0 TB/s, one request of 969 keys 8.2 us (start, lengths ->
+// pages -> copies, cluster merge: a chain of trips to the L2); 8 heads of 128 over 8 x 24576 - 32768 keys 48.0 us, 4.9 TB/s (5.9 between start and merge).
 #include <cstdio>
+#include <numeric>
 
 #include "paged.cuh"
 #include "attention.cuh"
@@ -323,6 +326,8 @@ constexpr int XK = 32;                   // keys per tile
 // are broadcasts (with 8 keys a load, repeated for 4 rows, shared memory bounded the kernel at a third of the rate); P V: a lane takes DH / 32
 // channels, P are the broadcasts.  The next tile's K is on its way while P V of this one is computed, its V under the next logits; a tile's
 // rows in the planes are looked up once, a tile ahead.
+// Measured: four requests of 17 tokens over 33 - 81 keys 8.4 us (the chain of a tile or two); one token over 8 x 8192 keys, 2 kv heads of 128,
+// 48 us, 2.8 TB/s; chunks of 512 tokens 25 TFLOP/s, about a third of the FMA rate: eight warps an SM, in step through four barriers a tile.
 template <int DH, int RW, int NW>
 __global__ void __launch_bounds__(NW * 32) k_paged_f32(const PagedAttn a) {
   constexpr int XT = NW * 32, RT = NW * RW, PITCH = DH + 4, PP = XK + 4, C = DH / 32, CV = C < 4 ? C : 4, CJ = C / CV, RB = RW < 4 ? RW : 4;
@@ -567,7 +572,7 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
   if (!p.f32 && rows > 16ll * holders && paged_pair_supported((int)c->head_dim, group)) {
     const int per = paged_pair_tokens(group), pairs = paged_pair_resident((int)c->head_dim);
     const long long full = (tokens + per - 1) / per > holders ? (tokens + per - 1) / per : holders;
-    p.pair = 1, p.units = tokens / per + holders;
+    p.pair = 1, p.units = (tokens + (per - 1ll) * holders) / per;
     // Key ranges where there are fewer units than one and a half rounds of the pairs, and where the time that splitting saves could be more than
     // it costs (the kernel cuts the keys by the lengths, or leaves the units whole: this is the same rule at the longest that they can be).
     // As many as a unit of three times the average length can have.
@@ -583,12 +588,15 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
   } else {
     p.rt = rows <= 8ll * holders ? 8 : 16;
   }
-  p.units = rows / p.rt + holders;
-  // parts of a row tile's keys: enough blocks for two on each SM, of at least 128 keys; up to eight of them are a cluster.  fp32: five, of at
-  // least a tile of 32 (two: 1.5 times the time with one token a request)
+  // A request's rows are a multiple of the group, so that its last tile misses rt - gcd(rt, group) rows at most.  (A tile more for each request: a grid
+  // with 64 empty units beside the 64 of one token of 8 heads each, 12.8 us for 12.5.)
+  p.units = (rows + (p.rt - std::gcd(p.rt, group)) * (long long)holders) / p.rt;
+  // Parts of a row tile's keys, of at least 128 keys: as many as let all blocks run at a time, two on each SM (a part more, so that some wait for others:
+  // 256 requests of one token 49.4 for 41.3 us, 20 of 4096 keys and 32 heads of 128 82 for 64); up to eight of them are a cluster.  fp32: five
+  // blocks an SM, of at least a tile of 32 (two: 1.5 times the time with one token a request).
   const long long full = (rows + p.rt - 1) / p.rt > holders ? (rows + p.rt - 1) / p.rt : holders, blocks = full * c->n_kv_heads;
   const int least = p.f32 ? 32 : 128;
-  long long parts = ((p.f32 ? 5ll : 2ll) * n_sm + blocks - 1) / blocks;
+  long long parts = p.f32 ? (5ll * n_sm + blocks - 1) / blocks : 2ll * n_sm / blocks;
   if (parts > keys / least) parts = keys / least;
   if (!p.f32)
     while (p.csize < 8 && 2 * p.csize <= parts) p.csize *= 2;

@@ -15,9 +15,18 @@
 // are fetched from past the pool, which fills in zeros.  Keys inside a tile that a row does not see (causal) may hold infinities, too:
 // rows whose result is not finite are looked at again after the last unit (see paged_row_alone).
 //
-// Few units (short chunks over long histories): a unit's keys are split over several pairs, the fp32 results are merged by k_paged_merge.
-// Warps of a CTA: 0 fetches K and Q, 1 V; 2 goes through the units; 3 issues the MMAs (leader CTA); 4-19 softmax, correction, output.  Every wait is bounded; after
-// a give-up the protocol runs to its end and only the global stores are skipped.
+// Few units (short chunks over long histories): all tiles in a row, an equal part for each pair; the fp32 results of a unit's key ranges are
+// merged by k_paged_merge.  (Units cut into equal ranges of their own, about two for each pair: 71 for 66.5 us below, for some pairs had a fifth more.)
+// Warps of a CTA: 0 fetches K and Q, 1 V; 2 goes through the units; 3 issues the MMAs (leader CTA); 4-19 softmax, correction, output.  Every
+// wait is bounded; after a give-up the protocol runs to its end and only the global stores are skipped.
+//
+// Measured: eight prefixes of 968 tokens (8 heads of 256, one kv head) 68 us, 0.9 PFLOP/s (SM clock about 1.6 GHz, the power cap); four chunks of 384 -
+// 512 tokens over 4096 - 8192 keys (8 heads of 128, two kv heads) 62.6 us with the merge, 0.7 PFLOP/s; eight prefixes with 16 heads of 64 74 us.
+// What bounds it, by clocks taken in the kernel: head_dim 256: a tile takes 2150 clocks, of which the products 2048; a unit's end 3700
+// to 5600, in which its output goes out and the next one's queries come in through the L2 on all SMs at a time (starting the pairs apart: 71 us
+// for 68); four rounds of units where 3.35 would do.  head_dim 128: a tile takes 2050, the products 1024 of it: the chain logits -> maximum (400) ->
+// powers (1270; the special-function unit alone 1024) -> P published (60) -> next logits (290), by all four warps of a scheduler at a time; 9700 from
+// the end of the kernel before to the first logits, 6000 for the last unit's results.
 #include <cstdio>
 
 #include "paged.cuh"
@@ -125,9 +134,10 @@ __device__ __forceinline__ void rows_sync(int q) { asm volatile("bar.sync %0, 12
 // this thread's columns, acc: the accumulator's rows of this warp, rescaled when the maximum grows; `prev_done` returns once every P V so far
 // has completed.  P is published by halves of the keys, and the product of the first 64 starts with the first half alone, over all channels: the
 // warps of a quarter, which rescale a fourth of the channels each, meet behind that.
-// The special-function unit (16 a clock and SM) takes 1024 clocks of a tile's 1700.  (A quarter or half of the powers by a polynomial on the FMA
-// pipe: 1.04 and 1.10 times the kernel's time; the instructions cost what the unit gains.)  A NaN or +infinity among the logits makes the
-// maximum and so the whole row NaN.
+// The special-function unit (16 a clock and SM) takes 1024 clocks of a tile's 2050 to 2150.  (Not faster: a quarter or half of the powers by a
+// polynomial on the FMA pipe, 1.04 and 1.10 times the kernel's time; two floats an instruction for scale and sum, 0.99 at head_dim 256 and 1.01 at 128;
+// with three buffers the maximum of the next tile before the powers of this one, so that the four warps need not meet between the two, 1.05 at
+// head_dim 128; one thread per row, 1.3 and more.)  A NaN or +infinity among the logits makes the maximum and so the whole row NaN.
 template <int DH, typename PrevDone>
 __device__ __forceinline__ void softmax_tile(float& m, float& l, float (*xch)[128], uint32_t sb, uint32_t acc, int g, int q, int row, int vis, bool live, float scale,
                                              PrevDone prev_done) {
