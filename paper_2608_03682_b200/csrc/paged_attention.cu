@@ -327,7 +327,8 @@ constexpr int XK = 32;                   // keys per tile
 // channels, P are the broadcasts.  The next tile's K is on its way while P V of this one is computed, its V under the next logits; a tile's
 // rows in the planes are looked up once, a tile ahead.
 // Measured: four requests of 17 tokens over 33 - 81 keys 8.4 us (the chain of a tile or two); one token over 8 x 8192 keys, 2 kv heads of 128,
-// 48 us, 2.8 TB/s; chunks of 512 tokens 25 TFLOP/s, about a third of the FMA rate: eight warps an SM, in step through four barriers a tile.
+// 42 us, 3.2 TB/s; 64 requests of 600 - 968 keys, 8 heads of 256: 54 us, 1.9 TB/s (every pair of rows reads the tile from shared memory; a row a warp
+// 48 and 62, four rows a warp 42 and 57); chunks of 512 tokens 25 TFLOP/s, about a third of the FMA rate: eight warps an SM, in step through four barriers a tile.
 template <int DH, int RW, int NW>
 __global__ void __launch_bounds__(NW * 32) k_paged_f32(const PagedAttn a) {
   constexpr int XT = NW * 32, RT = NW * RW, PITCH = DH + 4, PP = XK + 4, C = DH / 32, CV = C < 4 ? C : 4, CJ = C / CV, RB = RW < 4 ? RW : 4;
@@ -704,7 +705,7 @@ phyai_status_t phyai_paged_attention(const phyai_paged_cache_t* cache, uint32_t 
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaErrorInvalidValue;
   if (p.f32) {
-#define PHYAI_F32_ROWS(DH) (p.rt == 4 ? launch_f32<DH, 1, 4>(a, p, st) : p.rt == 8 ? launch_f32<DH, 1, 8>(a, p, st) : p.rt == 16 ? launch_f32<DH, 2, 8>(a, p, st) : launch_f32<DH, 8, 8>(a, p, st))
+#define PHYAI_F32_ROWS(DH) (p.rt == 4 ? launch_f32<DH, 2, 2>(a, p, st) : p.rt == 8 ? launch_f32<DH, 2, 4>(a, p, st) : p.rt == 16 ? launch_f32<DH, 2, 8>(a, p, st) : launch_f32<DH, 8, 8>(a, p, st))
     e = dh == 64 ? PHYAI_F32_ROWS(64) : dh == 128 ? PHYAI_F32_ROWS(128) : PHYAI_F32_ROWS(256);
 #undef PHYAI_F32_ROWS
   } else if (p.pair) {
