@@ -576,7 +576,7 @@ phyai_status_t phyai_append_paged_kv(const phyai_paged_cache_t *cache, const phy
  *   q           device, token rows of n_q_heads heads (a multiple of n_kv_heads; head h reads kv head h / (n_q_heads / n_kv_heads)), of the
  *               cache's type, q_stride elements apart, already rotated
  *   scale       of the logits; 0 = 1 / sqrt(head_dim)
- *   out         device, [tokens][n_q_heads][head_dim], the cache's type; overlaps no input
+ *   out         device, [tokens][n_q_heads][head_dim], the cache's type; overlaps no input (q from its first row to its last, the pages: refused)
  *   workspace   device, 16-byte aligned, phyai_paged_attention_workspace_bytes() bytes with the same sizes (on the same kind of device): this call's
  *               until its work has run.  Calls that may overlap (other streams, captured graphs replayed side by side) need one each
  */

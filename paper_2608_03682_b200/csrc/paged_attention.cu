@@ -14,7 +14,7 @@
 // The warps of a block merge through shared memory, the blocks of a cluster through distributed shared memory, several clusters of a
 // row (key ranges) through a second kernel.
 // Measured, one token a request: 8 heads of 256, 64 requests of 601 - 969 keys 12.5 us, 4.1 TB/s, 256 41 us, 5.0 TB/s, one request of 969 keys 8.2 us (start, lengths ->
-// pages -> copies, cluster merge: a chain of trips to the L2); 8 heads of 128 over 8 x 24576 - 32768 keys 48.0 us, 4.9 TB/s (5.9 between start and merge).
+// pages -> copies, cluster merge: a chain of trips to the L2); 8 heads of 128 over 8 x 24576 - 32768 keys 47.0 us, 5.0 TB/s (5.9 between start and merge).
 #include <cstdio>
 #include <numeric>
 
@@ -557,6 +557,26 @@ phyai_status_t bad_arg(const char* m) {
   return PHYAI_ERR_INVALID_ARG;
 }
 
+template <typename K>
+cudaError_t allow_smem(K kern, size_t bytes) { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); }
+
+// Clusters of 2^l blocks of k_paged_few that run at a time on the current device (all its forms have the same shared memory; 0: cannot be said).
+int few_active(int l) {
+  static PerDeviceCount n[4];
+  const int v = n[l].get([l] {
+    if (allow_smem(k_paged_few<256, 2>, Few<256>::SMEM) != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(1024), cfg.blockDim = dim3(FW * 32), cfg.dynamicSmemBytes = Few<256>::SMEM;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 1u << l, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    cfg.attrs = at, cfg.numAttrs = 1;
+    int active = 0;
+    return cudaOccupancyMaxActiveClusters(&active, k_paged_few<256, 2>, &cfg) == cudaSuccess ? active : 0;
+  });
+  return v > 0 ? v : 0;
+}
+
 // What a call launches: the kernel's row tile, its units and key ranges.
 struct Plan {
   int f32, pair, rt, ranges, csize;      // csize: blocks of a cluster, which share a range
@@ -592,25 +612,28 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
   // A request's rows are a multiple of the group, so that its last tile misses rt - gcd(rt, group) rows at most.  (A tile more for each request: a grid
   // with 64 empty units beside the 64 of one token of 8 heads each, 12.8 us for 12.5.)
   p.units = (rows + (p.rt - std::gcd(p.rt, group)) * (long long)holders) / p.rt;
-  // Parts of a row tile's keys, of at least 128 keys: as many as let all blocks run at a time, two on each SM (a part more, so that some wait for others:
-  // 256 requests of one token 49.4 for 41.3 us, 20 of 4096 keys and 32 heads of 128 82 for 64); up to eight of them are a cluster.  fp32: five
-  // blocks an SM, of at least a tile of 32 (two: 1.5 times the time with one token a request).
   const long long full = (rows + p.rt - 1) / p.rt > holders ? (rows + p.rt - 1) / p.rt : holders, blocks = full * c->n_kv_heads;
-  const int least = p.f32 ? 32 : 128;
-  long long parts = p.f32 ? (5ll * n_sm + blocks - 1) / blocks : 2ll * n_sm / blocks;
-  if (parts > keys / least) parts = keys / least;
-  if (!p.f32)
-    while (p.csize < 8 && 2 * p.csize <= parts) p.csize *= 2;
-  parts /= p.csize;
-  p.ranges = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+  if (p.f32) {
+    // Parts of a row tile's keys: five blocks an SM, of at least a tile of 32 (two: 1.5 times the time with one token a request)
+    long long parts = (5ll * n_sm + blocks - 1) / blocks;
+    if (parts > keys / 32) parts = keys / 32;
+    p.ranges = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    return p;
+  }
+  // A row tile's keys go to the largest cluster, of up to eight blocks with at least 128 keys each, that lets all tiles run at a time, and to as many of those
+  // (key ranges, merged by a second kernel) as run at a time.  What does is asked of the device: 296 blocks, but 33 clusters of eight (one more and its keys
+  // wait for a whole round: 18 requests of 4000 - 5000 keys, two clusters each, 27.1 us for 19.0 with one; 36 of 600 - 969 keys 19.4 for 11.9 with
+  // four blocks each; 256 of one block each 41, of two 49).  Clusters before ranges: 64 requests 12.5 us for 14.8 and more.
+  int most = few_active(0);
+  for (int l = 1; l <= 3 && (128ll << l) <= keys && blocks <= few_active(l); ++l) p.csize = 1 << l, most = few_active(l);
+  long long ranges = most / blocks;
+  if (ranges > keys / (128 * p.csize)) ranges = keys / (128 * p.csize);
+  p.ranges = (int)(ranges < 1 ? 1 : ranges > 64 ? 64 : ranges);
   return p;
 }
 size_t partial_bytes(const Plan& p, int hq, int dh, int tokens) {
   return p.ranges > 1 ? (size_t)p.ranges * tokens * hq * ((size_t)dh * 4 + 16) + 16 : 0;      // (16: the accumulators begin on 32 bytes)
 }
-
-template <typename K>
-cudaError_t allow_smem(K kern, size_t bytes) { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); }
 
 template <int DH, int NT>
 cudaError_t launch_few(const PagedAttn& a, const Plan& p, const CUtensorMap& map, cudaStream_t st) {
@@ -660,7 +683,9 @@ size_t phyai_paged_attention_workspace_bytes(const phyai_paged_cache_t* cache, u
                                              uint32_t max_pages) {
   using namespace phyai;
   const int n_sm = paged_sm_count();
-  if (!cache || !cache->n_kv_heads || !n_q_heads || !tokens || !batch || n_sm <= 0) return 0;
+  // (0 for calls that phyai_paged_attention refuses)
+  if (!cache || !cache->n_kv_heads || !n_q_heads || n_q_heads % cache->n_kv_heads || !tokens || !batch || batch > (uint32_t)PAGED_MAX_BATCH || n_sm <= 0) return 0;
+  if ((uint64_t)tokens * (n_q_heads / cache->n_kv_heads) > 0x7fffffffull || (uint64_t)max_pages * cache->page_size > 0x7fffffffull) return 0;
   return partial_bytes(make_plan(cache, (int)n_q_heads, (int)tokens, (int)batch, (int)max_pages, n_sm), (int)n_q_heads, (int)cache->head_dim, (int)tokens);
 }
 
@@ -683,6 +708,13 @@ phyai_status_t phyai_paged_attention(const phyai_paged_cache_t* cache, uint32_t 
   if (((reinterpret_cast<uintptr_t>(status_word) | reinterpret_cast<uintptr_t>(prefix_lens)) & 3u)) return bad_arg("status_word and prefix_lens must be 4-byte aligned");
   if ((uint64_t)tokens * (n_q_heads / cache->n_kv_heads) > 0x7fffffffull) return bad_arg("tokens too large");
   if (!tokens) return PHYAI_OK;
+  auto overlap = [&](const void* p, uint64_t bytes) {      // out and what is read
+    const uint64_t o = reinterpret_cast<uintptr_t>(out), i = reinterpret_cast<uintptr_t>(p);
+    return o < i + bytes && i < o + (uint64_t)tokens * n_q_heads * cache->head_dim * es;
+  };
+  if (overlap(q, ((tokens - 1ull) * q_stride + (uint64_t)n_q_heads * cache->head_dim) * es) ||
+      overlap(cache->pages, 2ull * cache->n_layers * cache->n_pages * cache->page_size * cache->n_kv_heads * cache->head_dim * es))
+    return bad_arg("out overlaps q or the pages");
   const int n_sm = paged_sm_count();
   if (n_sm <= 0) {
     snprintf(g_paged_err, sizeof(g_paged_err), "no CUDA device (there is no CPU fallback)");

@@ -299,6 +299,44 @@ def test_keys_that_a_row_does_not_see_have_no_part_in_it(dtype, value, Hq, Hkv, 
 
 
 @pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens", [
+    (8, 2, 128, [40] * 6, [6000, 300, 40, 2000, 100, 77]), (8, 1, 256, [64, 33], [5000, 33]), (4, 4, 64, [90, 1, 0, 17], [3000, 4000, 10, 17]),
+    (8, 1, 256, [300], [2100]), (8, 1, 128, [400, 3], [400, 5000]), (6, 2, 128, [0, 0, 100, 0], [50, 20000, 3000, 0]),
+])
+@pytest.mark.parametrize("mask", ["causal", "full", "prefix"])
+def test_attention_of_few_units_over_keys_of_any_lengths(Hq, Hkv, dh, q_lens, kv_lens, mask):
+    """All tiles in a row, an equal part for each pair of blocks: parts that begin and end inside a unit, that hold several, units of one part."""
+    prefix = [min(n, 70 * (i + 1)) for i, n in enumerate(kv_lens)] if mask == "prefix" else None
+    run_attention(Paged(37, q_lens, kv_lens, Hkv, dh, 64, first_row=2, last_rows=3), Hq, mask != "full", prefix)
+
+
+@pytest.mark.parametrize("seed", range(10))
+def test_attention_of_few_units_at_random_lengths(seed):
+    rng = np.random.default_rng(1000 + seed)
+    Hq, Hkv, dh = [(8, 1, 256), (8, 2, 128), (4, 2, 64), (32, 8, 128)][seed % 4]
+    kv = [int(2 ** rng.uniform(0, 12.5)) for _ in range(int(rng.integers(1, 7)))]
+    q = [int(rng.integers(0, min(n, 150) + 1)) for n in kv]
+    q[0] = max(q[0], 1)
+    run_attention(Paged(38 + seed, q, kv, Hkv, dh, [16, 32, 64, 128, 256][seed % 5]), Hq, seed % 3 != 0)
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens", [(8, 1, 256, [150, 20], [4000, 900]), (8, 2, 128, [90], [7000])])
+def test_keys_that_a_row_does_not_see_in_a_part_of_a_long_history(value, Hq, Hkv, dh, q_lens, kv_lens):
+    """The newer half of the new tokens' keys and values, in whole tiles and inside one, hidden from the older half's rows."""
+    p = Paged(39, q_lens, kv_lens, Hkv, dh, 32)
+    q = normal(p.rng, (p.T, Hq, dh)).cuda()
+    rows = []
+    for b, (n, kv) in enumerate(zip(q_lens, kv_lens)):
+        p.cache.pages[1, :, P.slots(p.table[b], 32, kv)[kv - n // 2:]] = value
+        rows += range(int(p.cu[b]), int(p.cu[b]) + n - n // 2)
+    got = p.cache.attend(1, q, *p.device_args())
+    assert p.cache.poll_status() == 0
+    planes = f64(p.cache.pages[1])
+    ref = P.attend(f64(q), planes[0], planes[1], p.cu, kv_lens, p.table, 32, True)
+    check_attention(f64(got)[rows], [r[rows] for r in ref], "bf16", dh, max(kv_lens))
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens", [
     (256, 1, 64, [1, 3], [40, 3]), (128, 1, 128, [2, 1], [200, 130]), (96, 1, 64, [5], [70]), (40, 4, 256, [30, 2], [131, 64]),
 ])
 def test_attention_of_wide_groups_of_heads(Hq, Hkv, dh, q_lens, kv_lens):

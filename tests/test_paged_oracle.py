@@ -65,7 +65,7 @@ def _heads(**kw):
 
 def _attend(lib, cache, **kw):
     a = dict(layer=0, hq=4, tokens=2, q=ADDRESS, q_stride=256, batch=1, cu=ADDRESS, lens=ADDRESS, table=ADDRESS, most=2, causal=1, prefix=None,
-             scale=0.0, out=ADDRESS, work=None, size=0, status=ADDRESS)
+             scale=0.0, out=2 * ADDRESS, work=None, size=0, status=ADDRESS)
     a.update(kw)
     return lib.phyai_paged_attention(C.byref(cache) if cache is not None else None, *list(a.values())[:-1], a["status"], None)
 
@@ -87,7 +87,7 @@ def test_caches_that_are_refused(lib, cache, status):
 @pytest.mark.parametrize("call", [
     dict(layer=2), dict(hq=0), dict(q=None), dict(q=ADDRESS + 2), dict(q_stride=255), dict(q_stride=260), dict(q_stride=192), dict(batch=0), dict(batch=1025),
     dict(cu=None), dict(lens=None), dict(table=None), dict(most=0), dict(causal=0, prefix=ADDRESS), dict(scale=-1.0), dict(scale=float("nan")),
-    dict(out=None), dict(out=ADDRESS + 4), dict(status=None), dict(most=1 << 28), dict(cu=ADDRESS + 2), dict(lens=ADDRESS + 1),
+    dict(out=None), dict(out=2 * ADDRESS + 4), dict(out=ADDRESS), dict(q=2 * ADDRESS - 1008), dict(out=ADDRESS + 32768 - 16), dict(status=None), dict(most=1 << 28), dict(cu=ADDRESS + 2), dict(lens=ADDRESS + 1),
     dict(table=ADDRESS + 3), dict(status=ADDRESS + 2), dict(prefix=ADDRESS + 2), dict(tokens=1 << 31),
 ])
 def test_attention_calls_that_are_refused(lib, call):
@@ -139,3 +139,9 @@ def test_pack_calls_that_are_refused(lib):
 def test_calls_without_tokens_do_nothing(lib):
     assert _attend(lib, _cache(), tokens=0, q=None, out=None) == binding.OK
     assert lib.phyai_paged_attention_workspace_bytes(C.byref(_cache()), 4, 0, 1, 2) == 0
+
+
+def test_no_workspace_for_calls_that_are_refused(lib):
+    for c, *a in ((_cache(), 4, 0xffffffff, 1, 2), (_cache(), 4, 0xffffffff, 0xffffffff, 2), (_cache(n_kv_heads=3), 4, 8, 1, 2), (_cache(n_kv_heads=8), 4, 8, 1, 2),
+                  (_cache(), 4, 8, 1025, 2), (_cache(page_size=0), 4, 8, 1, 0), (_cache(), 4, 8, 1, 0xffffffff), (_cache(n_kv_heads=0), 4, 8, 1, 2)):
+        assert lib.phyai_paged_attention_workspace_bytes(C.byref(c), *a) == 0
