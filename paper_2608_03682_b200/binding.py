@@ -659,7 +659,7 @@ class PagedCache:
         self._desc_ptr = C.addressof(self._desc)
         self.status = torch.zeros(1, dtype=torch.int32, device=pages.device)
         self._status_ptr = self.status.data_ptr()
-        self._work: Dict[tuple, int] = {}     # sizes of a call -> bytes of its workspace
+        self._sizes: Dict[tuple, int] = {}     # sizes of a call -> bytes of its workspace
 
     def poll_status(self) -> int:
         """Read-and-clear the status word (synchronises); returns the status code."""
@@ -724,12 +724,12 @@ class PagedCache:
             raise ValueError("out must be a contiguous tensor of q's shape and type")
         if scale is not None and not scale > 0.0:
             raise ValueError("scale must be positive")
-        need = self._work.get((Hq, T, B, most))
+        need = self._sizes.get((Hq, T, B, most))
         with _launch(device, stream) as sp:
             if need is None:
-                if len(self._work) >= 4096:
-                    self._work.clear()
-                need = self._work[Hq, T, B, most] = lib.phyai_paged_attention_workspace_bytes(self._desc_ptr, Hq, T, B, most)
+                if len(self._sizes) >= 4096:
+                    self._sizes.clear()
+                need = self._sizes[Hq, T, B, most] = lib.phyai_paged_attention_workspace_bytes(self._desc_ptr, Hq, T, B, most)
             work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
             if out is None:
                 out = _empty_rows(T, Hq, dh, self.dtype, device)
