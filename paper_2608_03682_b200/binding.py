@@ -507,49 +507,31 @@ _STORE = {torch.float32: DTYPES["f32"], torch.bfloat16: DTYPES["bf16"]}
 
 
 class _Elsewhere:
-    """A call on a given stream or another device: the device becomes the current one, outputs are allocated on the call's stream."""
+    """For a call on a given stream or another device: the device becomes the current one, outputs are allocated on the call's stream."""
 
     def __init__(self, device: torch.device, stream):
-        self.device, self.stream, self.raw = torch.cuda.device(device), torch.cuda.stream(stream), _raw_stream(stream, device)
+        if stream is not None and stream.device != device:
+            raise ValueError(f"the stream is not one of {device}")
+        self.device, self.stream = torch.cuda.device(device), torch.cuda.stream(stream)
 
     def __enter__(self):
         self.device.__enter__()
         self.stream.__enter__()
-        return self.raw
 
     def __exit__(self, *exc):
         self.stream.__exit__(*exc)
         self.device.__exit__(*exc)
 
 
-class _Here:
-    """The usual call: current device, current stream."""
-
-    def __init__(self, index: int):
-        self.index = index
-
-    def __enter__(self):
-        return torch._C._cuda_getCurrentRawStream(self.index)
-
-    def __exit__(self, *exc):
-        pass
-
-
-_HERE_ON = [_Here(i) for i in range(64)]
-
-
-def _launch(device: torch.device, stream):
-    i = device.index
-    return _HERE_ON[i] if stream is None and i < 64 and i == torch._C._cuda_getDevice() else _Elsewhere(device, stream)
-
-
 _I32, _F32 = torch.int32, torch.float32
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
-def _head_rows(name: str, t: torch.Tensor, device: torch.device, dtype: torch.dtype) -> tuple:
+# (devices are compared by index, -1: not a CUDA tensor: a call's checks take a good part of the time of its launch)
+def _head_rows(name: str, t: torch.Tensor, index: int, dtype: torch.dtype) -> tuple:
     """Checks rows of heads ``[T, heads, dh]`` (heads contiguous in a row); returns (T, heads, dh, row stride in elements)."""
-    if t.dtype is not dtype or t.device != device or t.dim() != 3:
-        raise ValueError(f"{name} must be a {dtype} tensor [tokens, heads, head_dim] on {device}")
+    if t.dtype is not dtype or t.get_device() != index or t.dim() != 3:
+        raise ValueError(f"{name} must be a {dtype} tensor [tokens, heads, head_dim] on cuda:{index}")
     T, H, dh = t.shape
     row, head, one = t.stride()
     if one != 1 or (head != dh and H > 1):
@@ -557,26 +539,26 @@ def _head_rows(name: str, t: torch.Tensor, device: torch.device, dtype: torch.dt
     return T, H, dh, row if T > 1 else H * dh
 
 
-def _ints(name: str, t: torch.Tensor, device: torch.device, shape: tuple) -> int:
-    if t.dtype is not _I32 or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
+def _ints(name: str, t: torch.Tensor, index: int, shape: tuple) -> int:
+    if t.dtype is not _I32 or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on cuda:{index}")
     return t.data_ptr()
 
 
-def _floats(name: str, t: Optional[torch.Tensor], device: torch.device, shape: tuple) -> Optional[int]:
+def _floats(name: str, t: Optional[torch.Tensor], index: int, shape: tuple) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype is not _F32 or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous float32 tensor {list(shape)} on {device}")
+    if t.dtype is not _F32 or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor {list(shape)} on cuda:{index}")
     return t.data_ptr()
 
 
-def _rope(t: Optional[torch.Tensor], device: torch.device, dh: int) -> tuple:
+def _rope(t: Optional[torch.Tensor], index: int, dh: int) -> tuple:
     """(address, positions) of a table of cosines and sines."""
     if t is None:
         return None, 0
     n = t.shape[0]
-    return _floats("rope_cos_sin", t, device, (n, dh // 2, 2)), n
+    return _floats("rope_cos_sin", t, index, (n, dh // 2, 2)), n
 
 
 def _empty_rows(T: int, H: int, dh: int, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
@@ -608,12 +590,16 @@ def norm_rope_heads(q: Optional[torch.Tensor], k: torch.Tensor, positions: Optio
     given).  ``status``: int32 word that a position outside the table raises (zeroed by the caller; None: a fresh one, not returned)."""
     lib = _lib or load_library()
     device, src = k.device, k.dtype
-    if src not in _STORE:
-        raise ValueError("k must be a float32 or bfloat16 tensor [tokens, heads, head_dim]")
-    T, Hkv, dh, k_row = _head_rows("k", k, device, src)
+    index = device.index
+    if src not in _STORE or index is None:
+        raise ValueError("k must be a float32 or bfloat16 CUDA tensor [tokens, heads, head_dim]")
+    if stream is not None or index != _current_device():
+        with _Elsewhere(device, stream):
+            return norm_rope_heads(q, k, positions, rope_cos_sin, q_gain, k_gain, eps, dtype, status)
+    T, Hkv, dh, k_row = _head_rows("k", k, index, src)
     Hq, q_row, q_ptr, q_out, q_out_ptr = 0, 0, None, None, None
     if q is not None:
-        Tq, Hq, dq, q_row = _head_rows("q", q, device, src)
+        Tq, Hq, dq, q_row = _head_rows("q", q, index, src)
         if Tq != T or dq != dh:
             raise ValueError("q and k differ in tokens or head_dim")
         q_ptr = q.data_ptr()
@@ -622,18 +608,17 @@ def norm_rope_heads(q: Optional[torch.Tensor], k: torch.Tensor, positions: Optio
     elif dtype not in _STORE:
         raise ValueError("dtype must be float32 or bfloat16")
     desc = _heads_desc(Hq, Hkv, dh, _STORE[src], _STORE[dtype], eps)
-    rope, n_pos = _rope(rope_cos_sin, device, dh)
-    gq, gk = _floats("q_gain", q_gain, device, (dh,)), _floats("k_gain", k_gain, device, (dh,))
-    pos = None if positions is None else _ints("positions", positions, device, (T,))
-    with _launch(device, stream) as sp:
-        if q is not None:
-            q_out = _empty_rows(T, Hq, dh, dtype, device)
-            q_out_ptr = q_out.data_ptr()
-        k_out = _empty_rows(T, Hkv, dh, dtype, device)
-        if status is None:
-            status = torch.zeros(1, dtype=torch.int32, device=device)
-        st = lib.phyai_norm_rope_heads(desc[1], T, q_ptr, q_row, k.data_ptr(), k_row, pos, rope, n_pos, gq, gk, q_out_ptr, k_out.data_ptr(),
-                                       _ints("status", status, device, (1,)), sp)
+    rope, n_pos = _rope(rope_cos_sin, index, dh)
+    gq, gk = _floats("q_gain", q_gain, index, (dh,)), _floats("k_gain", k_gain, index, (dh,))
+    pos = None if positions is None else _ints("positions", positions, index, (T,))
+    if q is not None:
+        q_out = _empty_rows(T, Hq, dh, dtype, device)
+        q_out_ptr = q_out.data_ptr()
+    k_out = _empty_rows(T, Hkv, dh, dtype, device)
+    if status is None:
+        status = torch.zeros(1, dtype=torch.int32, device=device)
+    st = lib.phyai_norm_rope_heads(desc[1], T, q_ptr, q_row, k.data_ptr(), k_row, pos, rope, n_pos, gq, gk, q_out_ptr, k_out.data_ptr(),
+                                   _ints("status", status, index, (1,)), _current_stream(index))
     if st != OK:
         _paged_fail(lib, st)
     return q_out, k_out
@@ -669,42 +654,44 @@ class PagedCache:
         return st
 
     def _requests(self, cu_q_lens, kv_lens, page_table):
-        device, shape = self.device, page_table.shape
+        index, shape = self.device.index, page_table.shape
         if len(shape) != 2:
             raise ValueError("page_table must be [batch, max_pages]")
         B, most = shape
-        return (B, most, None if cu_q_lens is None else _ints("cu_q_lens", cu_q_lens, device, (B + 1,)), _ints("kv_lens", kv_lens, device, (B,)),
-                _ints("page_table", page_table, device, shape))
+        return (B, most, None if cu_q_lens is None else _ints("cu_q_lens", cu_q_lens, index, (B + 1,)), _ints("kv_lens", kv_lens, index, (B,)),
+                _ints("page_table", page_table, index, shape))
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, cu_q_lens: torch.Tensor, kv_lens: torch.Tensor, page_table: torch.Tensor,
                rope_cos_sin: Optional[torch.Tensor], k_gain: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
                q_gain: Optional[torch.Tensor] = None, eps: float = 1e-6, positions: Optional[torch.Tensor] = None, stream=None):
         """New keys (normed with gain ``1 + k_gain`` unless None, rotated) and values ``[T, Hkv, dh]`` into the pages of ``layer``; with
         ``q`` ``[T, Hq, dh]`` returns its normed, rotated rows in the cache's type (rows of no request are not written), else None."""
-        lib, device, src = self.lib, self.device, k.dtype
+        lib, device, index, src = self.lib, self.device, self.device.index, k.dtype
         if src not in _STORE:
             raise ValueError("k must be a float32 or bfloat16 tensor [tokens, heads, head_dim]")
-        T, Hkv, dh, k_row = _head_rows("k", k, device, src)
-        Tv, Hv, dv, v_row = _head_rows("v", v, device, src)
+        if stream is not None or index != _current_device():
+            with _Elsewhere(device, stream):
+                return self.append(layer, k, v, cu_q_lens, kv_lens, page_table, rope_cos_sin, k_gain, q, q_gain, eps, positions)
+        T, Hkv, dh, k_row = _head_rows("k", k, index, src)
+        Tv, Hv, dv, v_row = _head_rows("v", v, index, src)
         if Tv != T or Hv != Hkv or dv != dh:
             raise ValueError("k and v differ in tokens, heads or head_dim")
         Hq, q_row, q_ptr, q_out, q_out_ptr = 0, 0, None, None, None
         if q is not None:
-            Tq, Hq, dq, q_row = _head_rows("q", q, device, src)
+            Tq, Hq, dq, q_row = _head_rows("q", q, index, src)
             if Tq != T or dq != dh:
                 raise ValueError("q and k differ in tokens or head_dim")
             q_ptr = q.data_ptr()
         desc = _heads_desc(Hq, Hkv, dh, _STORE[src], self._desc.dtype, eps)
         B, most, cu, lens, table = self._requests(cu_q_lens, kv_lens, page_table)
-        rope, n_pos = _rope(rope_cos_sin, device, dh)
-        gq, gk = _floats("q_gain", q_gain, device, (dh,)), _floats("k_gain", k_gain, device, (dh,))
-        pos = None if positions is None else _ints("positions", positions, device, (T,))
-        with _launch(device, stream) as sp:
-            if q is not None:
-                q_out = _empty_rows(T, Hq, dh, self.dtype, device)
-                q_out_ptr = q_out.data_ptr()
-            st = lib.phyai_append_paged_kv(self._desc_ptr, desc[1], layer, T, q_ptr, q_row, k.data_ptr(), k_row, v.data_ptr(), v_row, B, cu, lens, table,
-                                           most, pos, rope, n_pos, gq, gk, q_out_ptr, self._status_ptr, sp)
+        rope, n_pos = _rope(rope_cos_sin, index, dh)
+        gq, gk = _floats("q_gain", q_gain, index, (dh,)), _floats("k_gain", k_gain, index, (dh,))
+        pos = None if positions is None else _ints("positions", positions, index, (T,))
+        if q is not None:
+            q_out = _empty_rows(T, Hq, dh, self.dtype, device)
+            q_out_ptr = q_out.data_ptr()
+        st = lib.phyai_append_paged_kv(self._desc_ptr, desc[1], layer, T, q_ptr, q_row, k.data_ptr(), k_row, v.data_ptr(), v_row, B, cu, lens, table,
+                                       most, pos, rope, n_pos, gq, gk, q_out_ptr, self._status_ptr, _current_stream(index))
         if st != OK:
             _paged_fail(lib, st)
         return q_out
@@ -714,28 +701,30 @@ class PagedCache:
         """Attention of the new tokens' queries ``[T, Hq, dh]`` (rotated, the cache's type) over the pages of ``layer``, the tokens' own keys
         included.  ``causal``: a token sees what is cached before it and itself, and with ``prefix_lens`` (int32 ``[B]``) the first so many
         tokens.  Returns ``out`` ``[T, Hq, dh]`` (rows of no request are not written)."""
-        lib, device = self.lib, self.device
-        T, Hq, dh, row = _head_rows("q", q, device, self.dtype)
+        lib, device, index = self.lib, self.device, self.device.index
+        if stream is not None or index != _current_device():
+            with _Elsewhere(device, stream):
+                return self.attend(layer, q, cu_q_lens, kv_lens, page_table, causal, prefix_lens, scale, out)
+        T, Hq, dh, row = _head_rows("q", q, index, self.dtype)
         if dh != self.head_dim:
             raise ValueError("q and the cache differ in head_dim")
         B, most, cu, lens, table = self._requests(cu_q_lens, kv_lens, page_table)
-        prefix = None if prefix_lens is None else _ints("prefix_lens", prefix_lens, device, (B,))
+        prefix = None if prefix_lens is None else _ints("prefix_lens", prefix_lens, index, (B,))
         if out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != device or not out.is_contiguous()):
             raise ValueError("out must be a contiguous tensor of q's shape and type")
         if scale is not None and not scale > 0.0:
             raise ValueError("scale must be positive")
         need = self._sizes.get((Hq, T, B, most))
-        with _launch(device, stream) as sp:
-            if need is None:
-                if len(self._sizes) >= 4096:
-                    self._sizes.clear()
-                need = self._sizes[Hq, T, B, most] = lib.phyai_paged_attention_workspace_bytes(self._desc_ptr, Hq, T, B, most)
-            work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-            if out is None:
-                out = _empty_rows(T, Hq, dh, self.dtype, device)
-            st = lib.phyai_paged_attention(self._desc_ptr, layer, Hq, T, q.data_ptr(), row, B, cu, lens, table, most, 1 if causal else 0, prefix,
-                                           0.0 if scale is None else scale, out.data_ptr(), work.data_ptr() if need else None, need,
-                                           self._status_ptr, sp)
+        if need is None:
+            if len(self._sizes) >= 4096:
+                self._sizes.clear()
+            need = self._sizes[Hq, T, B, most] = lib.phyai_paged_attention_workspace_bytes(self._desc_ptr, Hq, T, B, most)
+        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        if out is None:
+            out = _empty_rows(T, Hq, dh, self.dtype, device)
+        st = lib.phyai_paged_attention(self._desc_ptr, layer, Hq, T, q.data_ptr(), row, B, cu, lens, table, most, 1 if causal else 0, prefix,
+                                       0.0 if scale is None else scale, out.data_ptr(), work.data_ptr() if need else None, need,
+                                       self._status_ptr, _current_stream(index))
         if st != OK:
             _paged_fail(lib, st)
         return out
@@ -745,15 +734,17 @@ class PagedCache:
         dh]``, ``cu_prefix_lens`` int32 ``[B + 1]``).  ``kv_tokens``: rows of it, at least the sum of ``kv_lens`` (rows past that are not
         written)."""
         lib, device = self.lib, self.device
+        if stream is not None or device.index != _current_device():
+            with _Elsewhere(device, stream):
+                return self.pack(page_table, kv_lens, kv_tokens, out)
         B, most, _, lens, table = self._requests(None, kv_lens, page_table)
         shape = (self.n_layers, 2, kv_tokens, self.n_kv_heads, self.head_dim)
         if out is not None and (out.shape != shape or out.dtype != self.dtype or out.device != device or not out.is_contiguous()):
             raise ValueError("out must be a contiguous tensor [L, 2, kv_tokens, Hkv, dh] of the cache's type")
-        with _launch(device, stream) as sp:
-            if out is None:
-                out = torch.empty(shape, dtype=self.dtype, device=device)
-            cu = torch.empty(B + 1, dtype=torch.int32, device=device)
-            st = lib.phyai_pack_paged_kv(self._desc_ptr, B, lens, table, most, out.data_ptr(), kv_tokens, cu.data_ptr(), self._status_ptr, sp)
+        if out is None:
+            out = torch.empty(shape, dtype=self.dtype, device=device)
+        cu = torch.empty(B + 1, dtype=torch.int32, device=device)
+        st = lib.phyai_pack_paged_kv(self._desc_ptr, B, lens, table, most, out.data_ptr(), kv_tokens, cu.data_ptr(), self._status_ptr, _current_stream(device.index))
         if st != OK:
             _paged_fail(lib, st)
         return out, cu

@@ -1,8 +1,10 @@
 """Pins of the paged-cache oracle by hand, and the refusals of the entry points (no GPU)."""
 import ctypes as C
+import types
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import paged_oracle as P
 from paper_2608_03682_b200 import binding, build
@@ -145,3 +147,8 @@ def test_no_workspace_for_calls_that_are_refused(lib):
     for c, *a in ((_cache(), 4, 0xffffffff, 1, 2), (_cache(), 4, 0xffffffff, 0xffffffff, 2), (_cache(n_kv_heads=3), 4, 8, 1, 2), (_cache(n_kv_heads=8), 4, 8, 1, 2),
                   (_cache(), 4, 8, 1025, 2), (_cache(page_size=0), 4, 8, 1, 0), (_cache(), 4, 8, 1, 0xffffffff), (_cache(n_kv_heads=0), 4, 8, 1, 2)):
         assert lib.phyai_paged_attention_workspace_bytes(C.byref(c), *a) == 0
+
+
+def test_a_stream_of_another_device_is_refused():
+    with pytest.raises(ValueError):
+        binding._Elsewhere(torch.device("cuda", 0), types.SimpleNamespace(device=torch.device("cuda", 1)))
