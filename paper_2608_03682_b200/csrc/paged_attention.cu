@@ -334,20 +334,24 @@ __global__ void __launch_bounds__(NW * 32) k_paged_f32(const PagedAttn a) {
   constexpr int XT = NW * 32, RT = NW * RW, PITCH = DH + 4, PP = XK + 4, C = DH / 32, CV = C < 4 ? C : 4, CJ = C / CV, RB = RW < 4 ? RW : 4;
   extern __shared__ __align__(16) uint8_t smem_raw[];
   __shared__ long long s_at[2][XK];        // element offset of a tile's keys in the planes, -1: none
+  __shared__ int s_skip;
   float* const Q = reinterpret_cast<float*>(smem_raw);
   float *const K = Q + RT * PITCH, *const V = K + XK * PITCH, *const P = V + XK * PITCH;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int hk = blockIdx.y;
   pdl_launch_dependents();
   pdl_wait();
+  // (the word is read by one thread: other blocks of the call may raise it at any time, and a block whose threads had read different
+  // values would go on with some of them, into barriers and shuffles of all)
+  if (tid == 0) s_skip = status_set(a.status);
+  __syncthreads();
   PagedRequest r;
   int tile;
-  const bool skip = status_set(a.status);
   if (!paged_unit<RT>(a, blockIdx.x, r, tile)) {
     if (tid == 0) atomicExch(a.status, ST_INVALID_ARG);
     return;
   }
-  if (r.b < 0 || skip) return;
+  if (r.b < 0 || s_skip) return;
   const int rows = min(RT, r.n * a.group - tile * RT), row0 = tile * RT;
   const int n_keys = r.limit((row0 + rows - 1) / a.group, a.causal);
   const int tiles = (n_keys + XK - 1) / XK, ranges = ranges_of(tiles, a.ranges, 1), range = blockIdx.z;
