@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(128) k_paged_merge(const PagedAttn a) {
   if (row >= rows) return;
   const int tok = (int)(row / a.hq);
   // (the lengths and the word say whether there is anything in the workspace; its entries are on their way meanwhile)
-  const bool live = !status_set(a.status) && tok >= a.pb.cu[0] && tok < a.pb.cu[a.pb.batch];
+  const bool mine = !status_set(a.status) && tok >= a.pb.cu[0] && tok < a.pb.cu[a.pb.batch];
   float4 ml = lane < a.ranges ? a.part_ml[(size_t)lane * rows + row] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
   const float* p = a.part_o + (size_t)row * DH + c;
   float x[4][C];
@@ -518,8 +518,9 @@ __global__ void __launch_bounds__(128) k_paged_merge(const PagedAttn a) {
     }
   };
   load(x[0], 0), load(x[1], 1);                             // (where a row has ranges it has two; a.ranges > 1: there is memory to read)
-  if (!live) return;
-  const int ranges = (int)__shfl_sync(0xffffffffu, ml.z, 0);
+  if (!__all_sync(0xffffffffu, mine)) return;               // (the warp as one: the word may change under it)
+  // (bounded: where the word was up for the kernel before and is not now, the workspace holds anything)
+  const int ranges = min((int)__shfl_sync(0xffffffffu, ml.z, 0), a.ranges);
   if (ranges <= 1) return;
   float4 ml2 = make_float4(-INFINITY, 0.f, 0.f, 0.f);       // (up to 64 ranges)
   if (lane + 32 < ranges) ml2 = a.part_ml[(size_t)(lane + 32) * rows + row];

@@ -29,3 +29,23 @@ def test_fp32_blocks_that_begin_while_others_raise_the_word(q_len):
         p.cache.attend(0, q, *args[:2], bad)
         assert p.cache.poll_status() == binding.ERR_INVALID_ARG
     assert torch.equal(want, p.cache.attend(0, q, *args)) and p.cache.poll_status() == 0
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens,dtype", [(8, 2, 128, [1, 1], [9001, 3000], "bf16"), (8, 1, 256, [40], [2500], "bf16"),
+                                                            (8, 2, 128, [1, 2], [900, 300], "f32")])
+def test_the_word_changes_under_calls_that_run(Hq, Hkv, dh, q_lens, kv_lens, dtype):
+    """The second kernel of split calls reads the word, too; whatever it finds while another stream writes it, the call ends, reads nothing outside
+    its workspace (filled here with what would be 2^30 key ranges) and later ones are right."""
+    p = Paged(82, q_lens, kv_lens, Hkv, dh, 64, dtype)
+    q, args, side = normal(p.rng, (p.T, Hq, dh), dtype).cuda(), p.device_args(), torch.cuda.Stream()
+    want = p.cache.attend(1, q, *args)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for _ in range(20):
+            torch.full((1 << 22,), float(1 << 30), device="cuda")       # (freed: the next call's workspace)
+            p.cache.attend(1, q, *args)
+            with torch.cuda.stream(side):
+                p.cache.status.fill_(binding.ERR_INVALID_ARG)
+                p.cache.status.zero_()
+        torch.cuda.synchronize()
+    assert torch.equal(want, p.cache.attend(1, q, *args)) and p.cache.poll_status() == 0
