@@ -518,7 +518,8 @@ phyai_status_t phyai_batcher_plan(const phyai_batcher_config_t *cfg, uint32_t n,
  *   status_word device int32, zeroed by the caller; a violation found on the device sets it to PHYAI_ERR_INVALID_ARG.  Lengths out of
  *               order: the call writes nothing.  A table entry that names no page, a position outside the rotary table: nothing outside the
  *               buffers is read or written, what the call writes for the tokens or requests concerned is not specified.  A call that finds the
- *               word raised writes nothing.  (PHYAI_ERR_TIMEOUT: a bounded wait inside a kernel expired.)
+ *               word raised writes nothing.  PHYAI_ERR_TIMEOUT: a bounded wait inside a kernel expired; what that
+ *               call wrote is not specified.
  * The calls only enqueue work on `stream` (of the current device) and allocate nothing.  Errors: INVALID_ARG, UNSUPPORTED, CUDA; message in
  * phyai_paged_last_error().
  */
@@ -595,6 +596,10 @@ phyai_status_t phyai_paged_attention(const phyai_paged_cache_t *cache, uint32_t 
 phyai_status_t phyai_pack_paged_kv(const phyai_paged_cache_t *cache, uint32_t batch, const int32_t *kv_lens, const int32_t *page_table,
                                    uint32_t max_pages, void *prefix_kv, uint64_t kv_tokens, int32_t *cu_prefix_lens, int32_t *status_word,
                                    void *stream);
+
+/* Option of the paged cache's calls from now on, of the whole process (testing).  key "wait_limit": iteration bound of the kernels' waits, 1 .. 2^30
+ * (default 2^22).  Unknown key -> INVALID_ARG. */
+phyai_status_t phyai_paged_set_option(const char *key, int64_t value);
 
 /* Thread-local description of the last error of an entry point of the paged cache. */
 const char *phyai_paged_last_error(void);

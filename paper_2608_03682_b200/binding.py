@@ -33,7 +33,7 @@ EXPORTS = ("phyai_expert_create", "phyai_expert_destroy", "phyai_prefix_kv_bytes
            "phyai_batcher_destroy", "phyai_batcher_submit", "phyai_batcher_next", "phyai_batcher_pending",
            "phyai_batcher_plan", "phyai_w8a8_project", "phyai_w8a8_last_error", "phyai_project_features_kv", "phyai_kv_projector_create",
            "phyai_kv_projector_run", "phyai_kv_projector_destroy", "phyai_norm_rope_heads", "phyai_append_paged_kv", "phyai_paged_attention",
-           "phyai_paged_attention_workspace_bytes", "phyai_pack_paged_kv", "phyai_paged_last_error")
+           "phyai_paged_attention_workspace_bytes", "phyai_pack_paged_kv", "phyai_paged_set_option", "phyai_paged_last_error")
 
 
 class PhyaiError(RuntimeError):
@@ -157,6 +157,7 @@ def load_library() -> C.CDLL:
     lib.phyai_paged_attention_workspace_bytes.argtypes = [_VP, u32, u32, u32, u32]
     lib.phyai_paged_attention_workspace_bytes.restype = C.c_size_t
     lib.phyai_pack_paged_kv.argtypes = [_VP, u32, _VP, _VP, u32, _VP, u64, _VP, _VP, _VP]
+    lib.phyai_paged_set_option.argtypes = [C.c_char_p, C.c_int64]
     lib.phyai_paged_last_error.restype = C.c_char_p
     _lib = lib
     return lib
@@ -622,6 +623,14 @@ def norm_rope_heads(q: Optional[torch.Tensor], k: torch.Tensor, positions: Optio
     if st != OK:
         _paged_fail(lib, st)
     return q_out, k_out
+
+
+def set_paged_option(key: str, value: int):
+    """Option of the paged cache's calls (``phyai_paged_set_option``; testing)."""
+    lib = _lib or load_library()
+    st = lib.phyai_paged_set_option(key.encode(), int(value))
+    if st != OK:
+        _paged_fail(lib, st)
 
 
 class PagedCache:

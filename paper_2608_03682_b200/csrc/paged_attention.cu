@@ -15,7 +15,9 @@
 // row (key ranges) through a second kernel.
 // Measured, one token a request: 8 heads of 256, 64 requests of 601 - 969 keys 12.5 us, 4.1 TB/s, 256 41 us, 5.0 TB/s, one request of 969 keys 8.2 us (start, lengths ->
 // pages -> copies, cluster merge: a chain of trips to the L2); 8 heads of 128 over 8 x 24576 - 32768 keys 47.0 us, 5.0 TB/s (5.9 between start and merge).
+#include <atomic>
 #include <cstdio>
+#include <cstring>
 #include <numeric>
 
 #include "paged.cuh"
@@ -159,6 +161,7 @@ __global__ void __launch_bounds__(FW * 32, 2) k_paged_few(const PagedAttn a, con
     const int jk = 2 * it, jv = jk + 1, key0 = (t0 + warp + it * FW) << 4;
     const uint32_t ks = ring + (uint32_t)(jk % NS) * F::TILE, vs = ring + (uint32_t)(jv % NS) * F::TILE;
     mbar_wait_drain(smem_u32(&full[warp][jk % NS]), (uint32_t)(jk / NS) & 1u, wc);
+    __syncwarp();                                                    // (lanes leave the wait one by one; what follows is of the whole warp)
     float s[NT][2][4] = {};
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
@@ -200,6 +203,7 @@ __global__ void __launch_bounds__(FW * 32, 2) k_paged_few(const PagedAttn a, con
       pf[nt][1] = transpose8x8(pack_bf16(x[2], x[3]));
     }
     mbar_wait_drain(smem_u32(&full[warp][jv % NS]), (uint32_t)(jv / NS) & 1u, wc);
+    __syncwarp();
     if (key0 + 16 > r.kv) {                                          // rows past the cached tokens hold anything: their values become zeros
       const int keep = r.kv - key0;
       for (int i = lane; i < (16 - keep) * (DH / 8); i += 32) {
@@ -557,6 +561,8 @@ __global__ void __launch_bounds__(128) k_paged_merge(const PagedAttn a) {
 // =============================================================================================
 // host side
 // =============================================================================================
+std::atomic<unsigned> g_wait_limit{1u << 22};      // of the kernels' waits on copies and MMAs (phyai_paged_set_option)
+
 phyai_status_t bad_arg(const char* m) {
   snprintf(g_paged_err, sizeof(g_paged_err), "%s", m);
   return PHYAI_ERR_INVALID_ARG;
@@ -684,6 +690,14 @@ bool paged_pool_map(void* map, const phyai_paged_cache_t* c, uint32_t rows, uint
 
 extern "C" {
 
+phyai_status_t phyai_paged_set_option(const char* key, int64_t value) {
+  using namespace phyai;
+  if (!key || strcmp(key, "wait_limit")) return bad_arg("unknown option");
+  if (value < 1 || value > (1ll << 30)) return bad_arg("wait_limit must be 1..2^30");
+  g_wait_limit.store((unsigned)value, std::memory_order_relaxed);
+  return PHYAI_OK;
+}
+
 size_t phyai_paged_attention_workspace_bytes(const phyai_paged_cache_t* cache, uint32_t n_q_heads, uint32_t tokens, uint32_t batch,
                                              uint32_t max_pages) {
   using namespace phyai;
@@ -737,7 +751,7 @@ phyai_status_t phyai_paged_attention(const phyai_paged_cache_t* cache, uint32_t 
   a.k_plane = (const char*)cache->pages + 2 * (size_t)layer * plane, a.v_plane = (const char*)a.k_plane + plane;
   a.prefix_lens = prefix_lens, a.causal = causal ? 1 : 0, a.hq = (int)n_q_heads, a.hkv = (int)cache->n_kv_heads, a.group = a.hq / a.hkv;
   a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)dh)) * LOG2E;
-  a.ranges = p.ranges, a.status = status_word, a.wait_limit = 1u << 22;
+  a.ranges = p.ranges, a.status = status_word, a.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
   a.part_ml = reinterpret_cast<float4*>(workspace), a.part_o = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(a.part_ml + (size_t)p.ranges * tokens * n_q_heads) + 31) & ~(uintptr_t)31);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaErrorInvalidValue;

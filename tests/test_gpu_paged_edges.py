@@ -49,3 +49,39 @@ def test_the_word_changes_under_calls_that_run(Hq, Hkv, dh, q_lens, kv_lens, dty
                 p.cache.status.zero_()
         torch.cuda.synchronize()
     assert torch.equal(want, p.cache.attend(1, q, *args)) and p.cache.poll_status() == 0
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# waits that run out (the data that they wait for does arrive: nothing hangs)
+# ------------------------------------------------------------------------------------------------------------------
+def expired(p, q, args, want, sure=True):
+    """``sure``: a wait does expire (with a tile or two for each warp all copies may have come by the second poll: the call is good then)."""
+    out = torch.full_like(q, 5.0)
+    torch.full((1 << 28,), 0, dtype=torch.uint8, device="cuda")         # keys and values come from memory
+    binding.set_paged_option("wait_limit", 1)
+    try:
+        p.cache.attend(1, q, *args, out=out)
+        torch.cuda.synchronize()
+    finally:
+        binding.set_paged_option("wait_limit", 1 << 22)
+    status = p.cache.status.item()
+    assert status == binding.ERR_TIMEOUT or not sure and status == binding.OK and torch.equal(want, out)
+    p.cache.status.fill_(binding.ERR_TIMEOUT)
+    out.fill_(5.0)
+    p.cache.attend(1, q, *args, out=out)                                # the word is up: nothing is written
+    assert (out == 5.0).all() and p.cache.poll_status() == binding.ERR_TIMEOUT and p.cache.poll_status() == 0
+    assert torch.equal(want, p.cache.attend(1, q, *args)) and p.cache.poll_status() == 0
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens", [
+    (8, 1, 256, [1], [969]), (8, 1, 256, [1] * 300, [200] * 300),       # a cluster of eight; blocks of their own
+    (8, 2, 128, [1, 1], [9001, 3000]), (4, 1, 64, [2] * 3, [4100, 17, 300]),       # key ranges
+    (8, 1, 256, [2], [3000]), (16, 1, 128, [1] * 80, [500] * 80),       # 16 rows
+    (4, 1, 64, [1] * 300, [2000] * 300),                                # thirty tiles a warp
+])
+def test_expired_waits_of_few_rows(Hq, Hkv, dh, q_lens, kv_lens):
+    p = Paged(83, q_lens, kv_lens, Hkv, dh, 64)
+    q, args = normal(p.rng, (p.T, Hq, dh)).cuda(), p.device_args()
+    want = p.cache.attend(1, q, *args)
+    assert p.cache.poll_status() == 0
+    expired(p, q, args, want, sure=sum(kv_lens) > 500000)

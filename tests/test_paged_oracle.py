@@ -152,3 +152,11 @@ def test_no_workspace_for_calls_that_are_refused(lib):
 def test_a_stream_of_another_device_is_refused():
     with pytest.raises(ValueError):
         binding._Elsewhere(torch.device("cuda", 0), types.SimpleNamespace(device=torch.device("cuda", 1)))
+
+
+def test_options(lib):
+    for key, value in ((b"wait_limit", 0), (b"wait_limit", -1), (b"wait_limit", 1 << 31), (b"other", 1), (None, 1)):
+        assert lib.phyai_paged_set_option(key, value) == BAD and lib.phyai_paged_last_error()
+    assert lib.phyai_paged_set_option(b"wait_limit", 1 << 22) == binding.OK
+    with pytest.raises(binding.PhyaiError):
+        binding.set_paged_option("wait_limit", 0)
