@@ -650,7 +650,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
       __threadfence();
       rows_sync(q);                           // (maxima beside a range's result: written by another warp of the quarter)
     }
-    if (a.causal && __any_sync(0xffffffffu, odd) && !*reinterpret_cast<volatile int*>(&abort_flag)) {
+    // (the warp as one: another warp may raise the flag under it)
+    if (a.causal && __any_sync(0xffffffffu, odd) && !__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&abort_flag) != 0)) {
       int at = s_list[2];
       for (Unit u = next_unit(at, s_list[0], s_list[1]); u.r.b >= 0; u = next_unit(at, s_list[0], s_list[1])) {
         const int n_rows = min(TOK, u.r.n - u.tok0 - half * TOK) * G, end = min((u.t0 + u.T) * KB, u.r.kv);

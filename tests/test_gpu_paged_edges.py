@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import paged_oracle as P
 from paper_2608_03682_b200 import binding
 from tests.test_gpu_paged import Paged, ints, normal
 
@@ -54,6 +55,10 @@ def test_the_word_changes_under_calls_that_run(Hq, Hkv, dh, q_lens, kv_lens, dty
 # ------------------------------------------------------------------------------------------------------------------
 # waits that run out (the data that they wait for does arrive: nothing hangs)
 # ------------------------------------------------------------------------------------------------------------------
+def same(a, b):
+    return torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
 def expired(p, q, args, want, sure=True):
     """``sure``: a wait does expire (with a tile or two for each warp all copies may have come by the second poll: the call is good then)."""
     out = torch.full_like(q, 5.0)
@@ -65,12 +70,12 @@ def expired(p, q, args, want, sure=True):
     finally:
         binding.set_paged_option("wait_limit", 1 << 22)
     status = p.cache.status.item()
-    assert status == binding.ERR_TIMEOUT or not sure and status == binding.OK and torch.equal(want, out)
+    assert status == binding.ERR_TIMEOUT or not sure and status == binding.OK and same(want, out)
     p.cache.status.fill_(binding.ERR_TIMEOUT)
     out.fill_(5.0)
     p.cache.attend(1, q, *args, out=out)                                # the word is up: nothing is written
     assert (out == 5.0).all() and p.cache.poll_status() == binding.ERR_TIMEOUT and p.cache.poll_status() == 0
-    assert torch.equal(want, p.cache.attend(1, q, *args)) and p.cache.poll_status() == 0
+    assert same(want, p.cache.attend(1, q, *args)) and p.cache.poll_status() == 0
 
 
 @pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens", [
@@ -85,3 +90,21 @@ def test_expired_waits_of_few_rows(Hq, Hkv, dh, q_lens, kv_lens):
     want = p.cache.attend(1, q, *args)
     assert p.cache.poll_status() == 0
     expired(p, q, args, want, sure=sum(kv_lens) > 500000)
+
+
+@pytest.mark.parametrize("hidden", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens", [
+    (8, 1, 256, [64, 33], [5000, 33]), (8, 2, 128, [40] * 6, [6000, 300, 40, 2000, 100, 77]), (4, 4, 64, [90, 1, 0, 17], [3000, 4000, 10, 17]),   # split units
+    (8, 1, 256, [300] * 9, [300] * 9), (8, 1, 128, [600] * 5, [600] * 5), (4, 1, 64, [700, 90], [700, 1000]),                                    # whole ones
+])
+def test_expired_waits_of_many_rows(Hq, Hkv, dh, q_lens, kv_lens, hidden):
+    """``hidden``: with values that some rows do not see and that make these look once more, behind the last unit."""
+    p = Paged(84, q_lens, kv_lens, Hkv, dh, 32)
+    if hidden:
+        for b, (n, kv) in enumerate(zip(q_lens, kv_lens)):
+            if n:
+                p.cache.pages[1, 1, P.slots(p.table[b], 32, kv)[-(n // 2 + 1):]] = float("inf")
+    q, args = normal(p.rng, (p.T, Hq, dh)).cuda(), p.device_args()
+    want = p.cache.attend(1, q, *args)
+    assert p.cache.poll_status() == 0
+    expired(p, q, args, want)
