@@ -656,10 +656,13 @@ class PagedCache:
         self._sizes: Dict[tuple, int] = {}     # sizes of a call -> bytes of its workspace
 
     def poll_status(self) -> int:
-        """Read-and-clear the status word (synchronises); returns the status code."""
+        """Read-and-clear the status word, once every call on the cache so far has run (waits for the device: calls may be on any stream, or
+        replayed from graphs); returns the status code."""
+        torch.cuda.synchronize(self.device)
         st = int(self.status.item())
         if st:
             self.status.zero_()
+            torch.cuda.current_stream(self.device).synchronize()       # (a next call may be on another stream)
         return st
 
     def _requests(self, cu_q_lens, kv_lens, page_table):

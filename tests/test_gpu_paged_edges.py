@@ -52,6 +52,24 @@ def test_the_word_changes_under_calls_that_run(Hq, Hkv, dh, q_lens, kv_lens, dty
     assert torch.equal(want, p.cache.attend(1, q, *args)) and p.cache.poll_status() == 0
 
 
+def test_poll_status_waits_for_calls_on_other_streams():
+    p = Paged(85, [1, 2], [50, 40], 1, 64, 16)
+    q, k, args = normal(p.rng, (p.T, 4, 64)).cuda(), normal(p.rng, (p.T, 1, 64)).cuda(), p.device_args()
+    table = p.table.copy()
+    table[:, :4] = -1
+    bad, side = ints(table), torch.cuda.Stream()
+    want = p.cache.attend(1, q, *args)
+    for call in (lambda: p.cache.attend(1, q, *args[:2], bad, stream=side), lambda: p.cache.append(0, k, k, *args[:2], bad, None, stream=side),
+                 lambda: p.cache.pack(bad, args[1], 90, stream=side)):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)                               # about 10 ms ahead of the call
+        call()
+        assert p.cache.poll_status() == binding.ERR_INVALID_ARG
+        got = p.cache.attend(1, q, *args, stream=side)                  # the word is down for any stream
+        assert p.cache.poll_status() == 0 and torch.equal(want, got)
+
+
 # ------------------------------------------------------------------------------------------------------------------
 # waits that run out (the data that they wait for does arrive: nothing hangs)
 # ------------------------------------------------------------------------------------------------------------------
