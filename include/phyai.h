@@ -544,7 +544,8 @@ typedef struct {
  * it): y = x / sqrt(mean(x^2) + eps) * (1 + gain), then (y_j, y_{j + dh/2}) rotated by the angle of the token's position.
  *   q, k        device, `tokens` rows of n_q_heads / n_kv_heads heads of head_dim, heads contiguous in a row, rows q_stride / k_stride
  *               elements apart (columns of a fused q|k|v matrix); q may be NULL: k only
- *   positions   device int32 [tokens], 0 <= position < n_positions (NULL without a table)
+ *   positions   device int32 [tokens], 0 <= position < n_positions (NULL without a table); the rows of a token whose position is not are NaN,
+ *               and the status word is raised (which this call does not read: it writes its rows whether the word is up or not)
  *   rope_cos_sin  device float32 [n_positions][head_dim/2][2] as phyai_suffix_attention takes it, or NULL: no rotation
  *   q_gain, k_gain  device float32 [head_dim], or NULL: no norm of those heads
  *   q_out, k_out  device, contiguous rows [tokens][heads][head_dim]; may be q / k themselves where type and stride are the same, and

@@ -588,7 +588,7 @@ def norm_rope_heads(q: Optional[torch.Tensor], k: torch.Tensor, positions: Optio
                     dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None, stream=None):
     """Norm (gain ``1 + gain``; None: no norm) of every head of ``q`` ``[T, Hq, dh]`` and ``k`` ``[T, Hkv, dh]`` with the rotation by
     ``positions`` (int32 ``[T]``) in the same pass; rows may be columns of a fused matrix.  Returns (q, k) in ``dtype`` (default: as
-    given).  ``status``: int32 word that a position outside the table raises (zeroed by the caller; None: a fresh one, not returned)."""
+    given).  The rows of a token whose position is outside the table are NaN; ``status``: int32 word that it raises as well (zeroed by the caller)."""
     lib = _lib or load_library()
     device, src = k.device, k.dtype
     index = device.index

@@ -83,15 +83,14 @@ constexpr int HT = 256, HB = 4;          // threads of a block, blocks of an SM
 template <int DH, typename IN, typename OUT, bool APPEND, int U>
 __global__ void __launch_bounds__(HT, HB) k_heads(const HeadsArgs a) {
   constexpr int C = Raw<IN>::N, HALF = DH / 2, LANES = HALF / C, HPS = 32 / LANES, APART = LANES * 2;           // lanes per head, heads per slot
-  __shared__ int s_cu[APPEND ? PAGED_MAX_BATCH + 1 : 1], s_kv[APPEND ? PAGED_MAX_BATCH : 1];
-  __shared__ int s_skip;
+  __shared__ int s_cu[APPEND ? PAGED_MAX_BATCH + 1 : 1], s_kv[APPEND ? PAGED_MAX_BATCH : 1], s_skip;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LANES, c = (lane % LANES) * 2;
   const int hq = a.q ? a.hq : 0, H = hq + a.hkv + (a.v ? a.hkv : 0), slots = (H + HPS - 1) / HPS;
   const int step = (int)gridDim.x * (HT / 32) * U, step_tok = step / slots, step_slot = step - step_tok * slots;
   pdl_launch_dependents();
   pdl_wait();
-  if (threadIdx.x == 0) s_skip = status_set(a.status);
   if constexpr (APPEND) {
+    if (threadIdx.x == 0) s_skip = status_set(a.status);
     bool bad = false;
     for (int i = threadIdx.x; i < a.pb.batch; i += HT) {
       const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1], kv = a.pb.kv_lens[i];
@@ -104,10 +103,8 @@ __global__ void __launch_bounds__(HT, HB) k_heads(const HeadsArgs a) {
       if (threadIdx.x == 0) atomicExch(a.status, ST_INVALID_ARG);
       return;
     }
-  } else {
-    __syncthreads();
+    if (s_skip) return;
   }
-  if (s_skip) return;
 
   const int s0 = ((int)blockIdx.x * (HT / 32) + warp) * U;
   for (int tok0 = s0 / slots, slot0 = s0 % slots; tok0 < a.tokens;) {
@@ -152,10 +149,8 @@ __global__ void __launch_bounds__(HT, HB) k_heads(const HeadsArgs a) {
           }
         } else if (a.rope) {
           pos = a.positions[tok];
-          if ((unsigned)pos >= (unsigned)a.n_positions) {
-            if (lane == 0) atomicExch(a.status, ST_INVALID_ARG);
-            ok = false;
-          }
+          ok = (unsigned)pos < (unsigned)a.n_positions;
+          if (!ok && lane == 0) atomicExch(a.status, ST_INVALID_ARG);
         }
         if (ok && a.rope) {
           const float* t = a.rope + ((size_t)pos * HALF + c) * 2;
@@ -193,7 +188,11 @@ __global__ void __launch_bounds__(HT, HB) k_heads(const HeadsArgs a) {
           y[i] = fmaf(t, sn[i], y[i] * cs[i]);
         }
       }
-      if (ok && kind < 3) {
+      if (!APPEND && !ok) {                                      // (whoever does not look at the word sees it)
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[i] = y[i] = NAN;
+      }
+      if ((ok || !APPEND) && kind < 3) {
         OUT* p = kind == 0 ? (OUT*)a.q_out + ((size_t)tok * a.hq + h) * DH
                  : APPEND  ? (OUT*)(kind == 1 ? a.k_plane : a.v_plane) + ((size_t)row * a.hkv + (kind == 1 ? h - hq : h - hq - a.hkv)) * DH
                            : (OUT*)a.k_out + ((size_t)tok * a.hkv + h - hq) * DH;

@@ -6,7 +6,7 @@ import torch
 
 from oracle import paged_oracle as P
 from paper_2608_03682_b200 import binding
-from tests.test_gpu_paged import Paged, ints, normal
+from tests.test_gpu_paged import EPS, TYPES, Paged, check_heads, ints, normal, rope_table
 
 pytestmark = pytest.mark.gpu
 
@@ -50,6 +50,24 @@ def test_the_word_changes_under_calls_that_run(Hq, Hkv, dh, q_lens, kv_lens, dty
                 p.cache.status.zero_()
         torch.cuda.synchronize()
     assert torch.equal(want, p.cache.attend(1, q, *args)) and p.cache.poll_status() == 0
+
+
+@pytest.mark.parametrize("src,dst", [("bf16", "bf16"), ("f32", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("T,Hq,Hkv,dh", [(6, 3, 1, 64), (5000, 8, 1, 256), (3000, 8, 2, 128)])
+def test_rows_of_positions_outside_the_table_are_nan_and_no_others(src, dst, T, Hq, Hkv, dh):
+    """With a word, with one that is up, and without."""
+    rng = np.random.default_rng(T + dh)
+    table, positions, g = rope_table(100, dh), rng.integers(0, 100, T), normal(rng, (dh,), "f32", 0.3)
+    q, k = normal(rng, (T, Hq, dh), src).cuda(), normal(rng, (T, Hkv, dh), src).cuda()
+    bad = rng.permutation(T)[:max(2, T // 50)]
+    positions[bad] = rng.choice([-1, 100, 2 ** 31 - 1, -2 ** 31], len(bad))
+    good = np.setdiff1d(np.arange(T), bad)
+    for status in (ints([0]), ints([binding.ERR_TIMEOUT]), None):
+        yq, yk = binding.norm_rope_heads(q, k, ints(positions), table.cuda(), g.cuda(), None, eps=EPS, dtype=TYPES[dst], status=status)
+        assert status is None or status.item() == binding.ERR_INVALID_ARG
+        assert torch.isnan(yq[bad]).all() and torch.isnan(yk[bad]).all()
+        check_heads(yq[good], q[good], g, table, positions[good], dst)
+        check_heads(yk[good], k[good], None, table, positions[good], dst)
 
 
 def test_poll_status_waits_for_calls_on_other_streams():
