@@ -301,12 +301,14 @@ __global__ void __launch_bounds__(PP_T) k_pack_pages(const uint4* pages, uint4* 
   for (int w = 0; w < PP_T / 32; ++w) before += s_part[0][w], total += s_part[1][w];
   bad |= total > kv_tokens;
   if (s_skip) return;
+  if (bad) {
+    if (first && tid == 0) atomicExch(status, ST_INVALID_ARG);
+    return;
+  }
   if (first && tid == 0) {
     if (b == 0) cu[0] = 0;
-    cu[b + 1] = (int)min(before + max(my_len, 0), 0x7fffffffLL);
-    if (bad) atomicExch(status, ST_INVALID_ARG);
+    cu[b + 1] = (int)(before + my_len);                     // (at most kv_tokens < 2^31)
   }
-  if (bad) return;
   uint4* const o = dst + ((size_t)blockIdx.y * kv_tokens + before) * row_chunks;
   for (;;) {
 #pragma unroll

@@ -70,6 +70,18 @@ def test_rows_of_positions_outside_the_table_are_nan_and_no_others(src, dst, T, 
         check_heads(yk[good], k[good], None, table, positions[good], dst)
 
 
+@pytest.mark.parametrize("lens,room", [([40, -1], 90), ([40, 16 * 5], 200), ([40, 50], 89), ([2 ** 31 - 1, 50], 90), ([-2 ** 31, 50], 90)])
+def test_pack_with_lengths_out_of_order_writes_nothing(lens, room):
+    p = Paged(86, [0, 0], [40, 50], 1, 64, 16)                          # (a table of four pages and one entry more)
+    p.table = p.table[:, :4]
+    out, cu = torch.full((2, 2, room, 1, 64), 9.0, dtype=torch.bfloat16, device="cuda"), ints([7, 7, 7])
+    kv, table = ints(lens), ints(p.table)
+    st = p.cache.lib.phyai_pack_paged_kv(p.cache._desc_ptr, 2, kv.data_ptr(), table.data_ptr(), 4, out.data_ptr(), room, cu.data_ptr(),
+                                         p.cache.status.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert st == binding.OK and p.cache.poll_status() == binding.ERR_INVALID_ARG
+    assert (out == 9.0).all() and cu.tolist() == [7, 7, 7]
+
+
 def test_poll_status_waits_for_calls_on_other_streams():
     p = Paged(85, [1, 2], [50, 40], 1, 64, 16)
     q, k, args = normal(p.rng, (p.T, 4, 64)).cuda(), normal(p.rng, (p.T, 1, 64)).cuda(), p.device_args()
