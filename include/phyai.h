@@ -592,7 +592,8 @@ phyai_status_t phyai_paged_attention(const phyai_paged_cache_t *cache, uint32_t 
 /*
  * Pages -> the ragged prefix cache: cached tokens 0 .. kv_lens[b] - 1 of request b, of every layer, go to rows cu[b] .. of prefix_kv
  * [n_layers][2][kv_tokens][n_kv_heads][head_dim]; cu_prefix_lens (device int32 [batch + 1], written) is the exclusive prefix sum of kv_lens.
- * Rows >= cu[batch] are left untouched.  sum(kv_lens) > kv_tokens: lengths out of order (nothing is written, cu_prefix_lens neither).  Bit-exact copy.
+ * Rows >= cu[batch] are left untouched.  sum(kv_lens) > kv_tokens: lengths out of order (nothing is written, cu_prefix_lens neither).  Bit-exact copy;
+ * prefix_kv overlaps no page (refused).
  */
 phyai_status_t phyai_pack_paged_kv(const phyai_paged_cache_t *cache, uint32_t batch, const int32_t *kv_lens, const int32_t *page_table,
                                    uint32_t max_pages, void *prefix_kv, uint64_t kv_tokens, int32_t *cu_prefix_lens, int32_t *status_word,

@@ -458,6 +458,9 @@ phyai_status_t phyai_pack_paged_kv(const phyai_paged_cache_t* cache, uint32_t ba
   const size_t row_bytes = (size_t)cache->n_kv_heads * cache->head_dim * (cache->dtype == PHYAI_F32 ? 4 : 2), chunks = row_bytes / 16;
   const size_t longest = (size_t)max_pages * cache->page_size < kv_tokens ? (size_t)max_pages * cache->page_size : kv_tokens;
   if (kv_tokens > 0x7fffffffull || (size_t)max_pages * cache->page_size * chunks > 0x7fffffffull) return bad_arg("kv_tokens or max_pages too large");
+  const uint64_t o = reinterpret_cast<uintptr_t>(prefix_kv), o_bytes = 2ull * cache->n_layers * kv_tokens * row_bytes;
+  const uint64_t i = reinterpret_cast<uintptr_t>(cache->pages), i_bytes = 2ull * cache->n_layers * cache->n_pages * cache->page_size * row_bytes;
+  if (o < i + i_bytes && i < o + o_bytes) return bad_arg("prefix_kv overlaps the pages");
   // (a block per chunk of a request of twice the average length; the blocks of longer ones take several: a table is as wide as the longest
   // request may become, and blocks without work are not free)
   const size_t likely = 2 * kv_tokens / batch + 64, gx = ((longest < likely ? longest : likely) * chunks + PP_CHUNK - 1) / PP_CHUNK;

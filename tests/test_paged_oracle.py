@@ -160,3 +160,13 @@ def test_options(lib):
     assert lib.phyai_paged_set_option(b"wait_limit", 1 << 22) == binding.OK
     with pytest.raises(binding.PhyaiError):
         binding.set_paged_option("wait_limit", 0)
+
+
+@pytest.mark.parametrize("dtype,bytes_of_a_row", [("bf16", 128), ("f32", 256)])
+def test_packing_into_the_pages_is_refused(lib, dtype, bytes_of_a_row):
+    pool, packed = 2 * 2 * 64 * bytes_of_a_row, 2 * 2 * 8 * bytes_of_a_row           # 2 layers of 4 pages of 16 rows; 8 rows
+    c = _cache(dtype=binding.DTYPES[dtype])
+    for at in (ADDRESS, ADDRESS + pool - 16, ADDRESS - packed + 16):
+        lib.phyai_pack_paged_kv(None, 0, None, None, 0, None, 0, None, None, None)
+        assert lib.phyai_pack_paged_kv(C.byref(c), 1, ADDRESS, ADDRESS, 2, at, 8, ADDRESS, ADDRESS, None) == BAD
+        assert b"overlaps" in lib.phyai_paged_last_error()
