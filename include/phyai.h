@@ -574,7 +574,7 @@ phyai_status_t phyai_append_paged_kv(const phyai_paged_cache_t *cache, const phy
  *   causal 0    limit = kv_lens[b]
  *   causal 1    limit = max(p + 1, prefix_lens[b]), at most kv_lens[b]; prefix_lens: device int32 [batch] or NULL (0): image and prompt
  *               tokens that see one another
- * A row that sees no key is zero; keys that a row does not see have no part in it, whatever they hold.
+ * A row that sees no key is zero (one whose keys all have the logit -infinity is NaN); keys that a row does not see have no part in it, whatever they hold.
  *   q           device, token rows of n_q_heads heads (a multiple of n_kv_heads; head h reads kv head h / (n_q_heads / n_kv_heads)), of the
  *               cache's type, q_stride elements apart, already rotated
  *   scale       of the logits; 0 = 1 / sqrt(head_dim)

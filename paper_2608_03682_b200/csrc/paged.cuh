@@ -50,10 +50,13 @@ struct PagedAttn {
   float scale_log2;       // softmax scale * log2(e)
   int ranges;             // most key ranges of a row
   float* part_o;          // [ranges][tokens][hq][dh]: unnormalised accumulators of a key range
-  float4* part_ml;        // [ranges][tokens][hq]: maximum (log2 units), sum, ranges of this row (in range 0's entry)
+  float4* part_ml;        // [ranges][tokens][hq]: maximum (log2 units), sum, ranges of this row, 1 if it sees a key
   int* status;
   unsigned wait_limit;
 };
+
+// 1 / (sum of a row's weights); 0 for a row that sees no key.  (A row all of whose keys have the logit -infinity sums to 0: its result is 0 / 0, NaN.)
+__device__ __forceinline__ float paged_inv(float sum, bool sees) { return sees ? 1.0f / sum : 0.f; }
 
 // A request's lengths, and how many keys its new token i sees: keys [0, limit).
 struct PagedRequest {

@@ -292,13 +292,14 @@ __global__ void __launch_bounds__(FW * 32, 2) k_paged_few(const PagedAttn a, con
     // (0 x infinity and 0 x NaN of keys that this row does not see, or of its own: told apart below)
     if (a.causal && !(fabsf(o.x) + fabsf(o.y) + fabsf(o.z) + fabsf(o.w) < INFINITY)) s_again[rr] = 1;
     const int tok = r.lo + (row0 + rr) / a.group, h = hk * a.group + (row0 + rr) % a.group;
+    const bool sees = r.limit((row0 + rr) / a.group, a.causal) > 0;
     if (ranges == 1) {
-      const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+      const float inv = paged_inv(sum, sees);
       *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + ((size_t)tok * a.hq + h) * DH + c) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
     } else {
       *reinterpret_cast<float4*>(a.part_o + (((size_t)range * a.pb.tokens + tok) * a.hq + h) * DH + c) = o;
     }
-    if (c == 0 && a.ranges > 1) a.part_ml[((size_t)range * a.pb.tokens + tok) * a.hq + h] = make_float4(M, sum, (float)ranges, 0.f);
+    if (c == 0 && a.ranges > 1) a.part_ml[((size_t)range * a.pb.tokens + tok) * a.hq + h] = make_float4(M, sum, (float)ranges, sees ? 1.f : 0.f);
   }
   // no block leaves while another reads its shared memory; and the rows below are written over all channels
   if (csize > 1) cluster_sync_all();
@@ -311,13 +312,14 @@ __global__ void __launch_bounds__(FW * 32, 2) k_paged_few(const PagedAttn a, con
     const int tok = r.lo + i, h = hk * a.group + (row0 + rr) % a.group, c = lane * (DH / 32);
     float o[DH / 32], M, sum;
     paged_row_alone<DH>(a, r.b, (const __nv_bfloat16*)a.q + tok * a.q_stride + (long long)h * DH, hk, c0 * 16, min(c1 * 16, r.limit(i, 1)), o, M, sum);
-    const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+    const bool sees = r.limit(i, 1) > 0;
+    const float inv = paged_inv(sum, sees);
 #pragma unroll
     for (int e = 0; e < DH / 32; ++e) {
       if (ranges == 1) ((__nv_bfloat16*)a.out)[((size_t)tok * a.hq + h) * DH + c + e] = __float2bfloat16_rn(o[e] * inv);
       else a.part_o[(((size_t)range * a.pb.tokens + tok) * a.hq + h) * DH + c + e] = o[e];
     }
-    if (lane == 0 && ranges > 1) a.part_ml[((size_t)range * a.pb.tokens + tok) * a.hq + h] = make_float4(M, sum, (float)ranges, 0.f);
+    if (lane == 0 && ranges > 1) a.part_ml[((size_t)range * a.pb.tokens + tok) * a.hq + h] = make_float4(M, sum, (float)ranges, sees ? 1.f : 0.f);
   }
 }
 
@@ -466,7 +468,7 @@ __global__ void __launch_bounds__(NW * 32) k_paged_f32(const PagedAttn a) {
     const int it = (row0 + wr + i) / a.group, tok = r.lo + it, h = hk * a.group + (row0 + wr + i) % a.group;
     const size_t slot = ((size_t)range * a.pb.tokens + tok) * a.hq + h;
     float* const dst = ranges == 1 ? (float*)a.out + ((size_t)tok * a.hq + h) * DH : a.part_o + slot * DH;
-    const float inv = ranges > 1 ? 1.0f : sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+    const float inv = ranges > 1 ? 1.0f : paged_inv(sum, lim[i] > 0);
     float fin = 0.f;
 #pragma unroll
     for (int j = 0; j < CJ; ++j) {
@@ -476,18 +478,18 @@ __global__ void __launch_bounds__(NW * 32) k_paged_f32(const PagedAttn a) {
       if constexpr (CV == 4) *reinterpret_cast<float4*>(dst + lane * 4 + 128 * j) = make_float4(o[0], o[1], o[2], o[3]);
       else *reinterpret_cast<float2*>(dst + lane * 2 + 64 * j) = make_float2(o[0], o[1]);
     }
-    if (lane == 0 && a.ranges > 1) a.part_ml[slot] = make_float4(m[i], sum, (float)ranges, 0.f);
+    if (lane == 0 && a.ranges > 1) a.part_ml[slot] = make_float4(m[i], sum, (float)ranges, lim[i] > 0 ? 1.f : 0.f);
     // (0 x infinity and 0 x NaN: see k_paged_few)
     if (!a.causal || __all_sync(0xffffffffu, fin == 0.f)) continue;
     const int lm = r.limit(it, 1);
     if (!paged_hidden_odd<DH / 32, float>(a, r.b, hk, DH, 0, max(t0 * XK, lm), min(t1 * XK, n_keys))) continue;
     float o[DH / 32], M, sm;
     paged_row_alone<DH>(a, r.b, (const float*)a.q + tok * a.q_stride + (long long)h * DH, hk, t0 * XK, min(t1 * XK, lm), o, M, sm);
-    const float w = ranges > 1 ? 1.0f : sm > 0.f || sm != sm ? 1.0f / sm : 0.f;
+    const float w = ranges > 1 ? 1.0f : paged_inv(sm, lm > 0);
     __syncwarp();                          // (behind the stores above, of other lanes)
 #pragma unroll
     for (int e = 0; e < DH / 32; ++e) dst[lane * (DH / 32) + e] = o[e] * w;
-    if (lane == 0 && ranges > 1) a.part_ml[slot] = make_float4(M, sm, (float)ranges, 0.f);
+    if (lane == 0 && ranges > 1) a.part_ml[slot] = make_float4(M, sm, (float)ranges, lm > 0 ? 1.f : 0.f);
   }
 }
 
@@ -526,6 +528,7 @@ __global__ void __launch_bounds__(128) k_paged_merge(const PagedAttn a) {
   // (bounded: where the word was up for the kernel before and is not now, the workspace holds anything)
   const int ranges = min((int)__shfl_sync(0xffffffffu, ml.z, 0), a.ranges);
   if (ranges <= 1) return;
+  const bool sees = __shfl_sync(0xffffffffu, ml.w, 0) != 0.f;
   float4 ml2 = make_float4(-INFINITY, 0.f, 0.f, 0.f);       // (up to 64 ranges)
   if (lane + 32 < ranges) ml2 = a.part_ml[(size_t)(lane + 32) * rows + row];
   if (lane >= ranges) ml = make_float4(-INFINITY, 0.f, 0.f, 0.f);
@@ -549,7 +552,7 @@ __global__ void __launch_bounds__(128) k_paged_merge(const PagedAttn a) {
       for (int e = 0; e < C; ++e) o[e] = fmaf(w, x[j][e], o[e]);
     }
   }
-  const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+  const float inv = paged_inv(sum, sees);
   OUT* dst = (OUT*)a.out + row * DH + c;
 #pragma unroll
   for (int e = 0; e < C; e += 2) {

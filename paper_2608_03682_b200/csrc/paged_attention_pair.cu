@@ -588,14 +588,15 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
       xsum[i & 1][g][row] = l;
       rows_sync(q);
       const float sum = (xsum[i & 1][0][row] + xsum[i & 1][1][row]) + (xsum[i & 1][2][row] + xsum[i & 1][3][row]);
-      const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+      const bool sees = live && me.r.limit(tok, a.causal) > 0;
+      const float inv = paged_inv(sum, sees);
       wait_warp(last_bar, last_par, wc);
       tc_fence_after();
       const bool okf = !skip && !*reinterpret_cast<volatile int*>(&abort_flag);
       const int first_tok = me.r.lo + me.tok0 + half * TOK, n_rows = okf ? min(TOK, me.r.n - me.tok0 - half * TOK) * G : 0;
       const bool whole = me.ranges == 1;
       const size_t slot = ((size_t)me.range * a.pb.tokens + first_tok + row_tok) * a.hq + me.hk * G + (row - row_tok * G);
-      if (g == 0 && a.ranges > 1 && row < n_rows) a.part_ml[slot] = make_float4(m, sum, (float)me.ranges, 0.f);
+      if (g == 0 && a.ranges > 1 && row < n_rows) a.part_ml[slot] = make_float4(m, sum, (float)me.ranges, sees ? 1.f : 0.f);
       __nv_bfloat16* ob = (__nv_bfloat16*)a.out + ((size_t)first_tok * a.hq + me.hk * G) * DH;
       float fin = 0.f;
 #pragma unroll 1
@@ -668,7 +669,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
           float o[DH / 32], M, sum;
           paged_row_alone<DH>(a, u.r.b, (const __nv_bfloat16*)a.q + tok * a.q_stride + (long long)head * DH, u.hk, u.t0 * KB, min(end, lim), o, M, sum);
           // (a key range's result is relative to the maximum that stands beside it)
-          const float w = u.ranges == 1 ? (sum > 0.f || sum != sum ? 1.0f / sum : 0.f) : M == -INFINITY ? 0.f : exp2f(M - a.part_ml[slot].x);
+          const float w = u.ranges == 1 ? paged_inv(sum, lim > 0) : M == -INFINITY ? 0.f : exp2f(M - a.part_ml[slot].x);
 #pragma unroll
           for (int e = 0; e < DH / 32; ++e) {
             const int c = lane * (DH / 32) + e - c0;

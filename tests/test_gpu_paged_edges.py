@@ -6,7 +6,7 @@ import torch
 
 from oracle import paged_oracle as P
 from paper_2608_03682_b200 import binding
-from tests.test_gpu_paged import EPS, TYPES, Paged, check_heads, ints, normal, rope_table
+from tests.test_gpu_paged import EPS, TYPES, Paged, check_attention, check_heads, f64, ints, normal, rope_table
 
 pytestmark = pytest.mark.gpu
 
@@ -156,3 +156,46 @@ def test_expired_waits_of_many_rows(Hq, Hkv, dh, q_lens, kv_lens, hidden):
     want = p.cache.attend(1, q, *args)
     assert p.cache.poll_status() == 0
     expired(p, q, args, want)
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# infinities and NaN among the keys that a row does see
+# ------------------------------------------------------------------------------------------------------------------
+FORMS = [(8, 1, 256, [1], [40], "bf16"), (8, 1, 256, [1] * 300, [20] * 300, "bf16"), (8, 2, 128, [1, 2], [9001, 30], "bf16"), (8, 1, 256, [2], [3000], "bf16"),
+         (8, 1, 128, [64, 3], [64, 200], "bf16"), (8, 1, 256, [40], [2500], "bf16"), (4, 1, 64, [700], [700], "bf16"),
+         (4, 1, 64, [1, 3], [50, 20], "f32"), (8, 2, 128, [1], [5000], "f32"), (4, 1, 64, [40], [300], "f32")]
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens,dtype", FORMS)
+def test_rows_all_of_whose_logits_are_minus_infinity(Hq, Hkv, dh, q_lens, kv_lens, dtype):
+    """0 / 0 is NaN, as in the formula; zero is the result of a row that sees no key.  The queries' first channel is 1, and the keys' -infinity in all keys of
+    the last request but its last one: rows that see that key have a finite logit."""
+    p = Paged(87, q_lens, kv_lens, Hkv, dh, 16, dtype)
+    b = len(kv_lens) - 1
+    p.cache.pages[1, 0, P.slots(p.table[b], 16, kv_lens[b])[:-1], :, 0] = -float("inf")
+    q = normal(p.rng, (p.T, Hq, dh), dtype).cuda()
+    q[:, :, 0] = 1.0
+    args = p.device_args()
+    got = p.cache.attend(1, q, *args)
+    assert p.cache.poll_status() == 0
+    planes = f64(p.cache.pages[1])
+    ref = P.attend(f64(q), planes[0], planes[1], p.cu, kv_lens, p.table, 16, True)
+    blind = np.arange(int(p.cu[b]), int(p.cu[b + 1]) - 1)               # rows of the last request that do not see its last key
+    rest = np.setdiff1d(np.arange(p.T), blind)
+    assert torch.isnan(got[blind]).all() and np.isnan(ref[0][blind]).all()
+    ref[2][rest] = np.nan_to_num(ref[2][rest], posinf=float(dh))        # (the sums |q k| of finite logits are below that)
+    check_attention(f64(got)[rest], [r[rest] for r in ref], dtype, dh, max(kv_lens))
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens,dtype", FORMS)
+def test_every_row_that_sees_nan_or_infinite_logits_is_nan(value, Hq, Hkv, dh, q_lens, kv_lens, dtype):
+    p = Paged(88, q_lens, kv_lens, Hkv, dh, 16, dtype)
+    b = len(kv_lens) - 1
+    first = kv_lens[b] - (q_lens[b] + 1) // 2                           # a key that the newer rows of the last request see
+    p.cache.pages[1, 0, P.slots(p.table[b], 16, kv_lens[b])[first]] = value
+    q = normal(p.rng, (p.T, Hq, dh), dtype).abs().cuda() + 0.25         # (positive: the logits are +infinity, not of either sign)
+    got = p.cache.attend(1, q, *p.device_args())
+    assert p.cache.poll_status() == 0
+    sees = np.arange(int(p.cu[b + 1]) - (q_lens[b] + 1) // 2, int(p.cu[b + 1]))
+    assert torch.isnan(got[sees]).all() and torch.isfinite(got[np.setdiff1d(np.arange(p.T), sees)]).all()
