@@ -509,17 +509,18 @@ phyai_status_t phyai_batcher_plan(const phyai_batcher_config_t *cfg, uint32_t n,
  *   head_dim    64, 128 or 256;  page_size  16, 32, 64, 128 or 256;  dtype  PHYAI_F32 or PHYAI_BF16
  * Requests of a call:
  *   cu_q_lens   device int32 [batch + 1], non-decreasing, cu[0] >= 0, cu[batch] <= tokens: request b's new tokens are token rows
- *               cu[b] .. cu[b + 1] - 1; token rows of no request are neither read nor written
+ *               cu[b] .. cu[b + 1] - 1; token rows of no request have no part in any result and are not written
  *   kv_lens     device int32 [batch]: cached tokens of request b WITH its new ones, which are the last; <= max_pages * page_size
  *   page_table  device int32 [batch][max_pages]: cached token t of request b is row page_table[b][t / page_size] * page_size +
  *               t % page_size of the planes; entries past a request's last page are not read
  *   batch <= 1024.  Requests may share pages that they only read; a page that two requests of an append write holds the tokens of
  *   either.
- *   status_word device int32, zeroed by the caller; a violation found on the device sets it to PHYAI_ERR_INVALID_ARG.  Lengths out of
- *               order: the call writes nothing.  A table entry that names no page, a position outside the rotary table: nothing outside the
- *               buffers is read or written, what the call writes for the tokens or requests concerned is not specified.  A call that finds the
- *               word raised writes nothing.  PHYAI_ERR_TIMEOUT: a bounded wait inside a kernel expired; what that
- *               call wrote is not specified.
+ *   status_word device int32, zeroed by the caller; a violation found on the device sets it to PHYAI_ERR_INVALID_ARG.
+ *               Lengths out of order: the call writes nothing.  A table entry that names no page, a position outside the rotary table: nothing
+ *               outside the buffers is read or written, what the call writes for the requests (append: tokens) concerned is not specified, and all
+ *               others get what they would have got.  PHYAI_ERR_TIMEOUT: a bounded wait inside a kernel expired; what that call wrote is not
+ *               specified.  A call that finds the word raised by an earlier one writes nothing (replays of a captured call count as one call
+ *               where an entry raised it).
  * The calls only enqueue work on `stream` (of the current device) and allocate nothing.  Errors: INVALID_ARG, UNSUPPORTED, CUDA; message in
  * phyai_paged_last_error().
  */

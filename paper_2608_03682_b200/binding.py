@@ -637,7 +637,8 @@ class PagedCache:
     """Pages of keys and values of every layer: ``pages`` ``[L, 2, n_pages * page_size, Hkv, dh]`` (the caller's, float32 or bfloat16).
     A call's requests: ``cu_q_lens`` int32 ``[B + 1]`` (rows of the new tokens), ``kv_lens`` int32 ``[B]`` (cached tokens with the new
     ones), ``page_table`` int32 ``[B, max_pages]``; see ``phyai.h``.  What a call finds wrong on the device raises the cache's status word
-    (``poll_status``), and later calls write nothing until it has been read.  Streams: calls on the cache are ordered by the caller."""
+    (``poll_status``), and later calls write nothing until it has been read; a table entry that names no page leaves the call's other requests
+    as they would be.  Streams: calls on the cache are ordered by the caller."""
 
     def __init__(self, pages: torch.Tensor, page_size: int):
         self.lib = load_library()

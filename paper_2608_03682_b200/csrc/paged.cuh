@@ -21,7 +21,33 @@ struct PagedBatch {
   int batch, tokens, max_pages;
   int page_shift;         // log2(page_size)
   int n_pages;
+  unsigned* raised_by;    // which call raised this call's status word for an entry, and this call (see paged_stopped)
+  unsigned call;
 };
+
+// The status word.  A call that finds it up writes nothing, but an entry that names no page (or a position outside the rotary table)
+// concerns one request alone: the others' blocks, which may begin after the word went up, and the merge go on.  So whoever raises the word for an
+// entry notes the call's number first, and blocks that find the word up look whether it was their own call.  The word itself stays what a
+// caller expects, and while it is down nothing more is read.  (Notes lie in a table of the device by the word's address, paged_call: two calls on
+// words that share a note, and that both meet such entries at a time, could at worst take their own word for an earlier call's.)
+__device__ __forceinline__ bool paged_stopped(const int* status, const PagedBatch& p) {
+  const int v = *reinterpret_cast<const volatile int*>(status);
+  if (v == ST_OK) return false;
+  if (v != ST_INVALID_ARG) return true;
+  __threadfence();
+  return *reinterpret_cast<const volatile unsigned*>(p.raised_by) != p.call;
+}
+__device__ __forceinline__ void paged_bad_entry(int* status, const PagedBatch& p) {
+  atomicExch(p.raised_by, p.call);
+  __threadfence();
+  atomicCAS(status, ST_OK, ST_INVALID_ARG);
+}
+// for lengths out of order (every block sees them by itself) and in calls that do not read the word: stops every other call
+__device__ __forceinline__ void paged_raise(int* status, const PagedBatch& p) {
+  atomicExch(p.raised_by, 0u);
+  __threadfence();
+  atomicExch(status, ST_INVALID_ARG);
+}
 
 // row of the planes that holds cached token t of request b, or -1 if its table entry names no page
 __device__ __forceinline__ long long paged_row(const PagedBatch& p, int b, int t) {
@@ -153,6 +179,8 @@ extern thread_local char g_paged_err[256];
 phyai_status_t check_paged(const phyai_paged_cache_t* c, uint32_t layer, uint32_t batch, const int32_t* cu, const int32_t* kv_lens,
                            const int32_t* table, uint32_t max_pages, uint32_t tokens, bool all_layers, PagedBatch* out);
 int paged_sm_count();
+// numbers the call and finds the note of its status word on the current device
+cudaError_t paged_call(const int32_t* status_word, PagedBatch* p);
 
 // Key ranges of a row tile: at least `least` tiles of keys each.
 __host__ __device__ __forceinline__ int ranges_of(int tiles, int most, int least) {

@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(FW * 32, 2) k_paged_few(const PagedAttn a, con
   PagedRequest r;
   int tile;
   if (!paged_unit<RT>(a, unit, r, tile)) {
-    if (threadIdx.x == 0) atomicExch(a.status, ST_INVALID_ARG);
+    if (threadIdx.x == 0) paged_raise(a.status, a.pb);
     return;
   }
   if (r.b < 0) return;
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(FW * 32, 2) k_paged_few(const PagedAttn a, con
     const int i = i0 + lane;
     page_of = i < mine ? a.pb.table[trow + ((t0 + warp + i * FW) << 4 >> a.pb.page_shift)] : 0;
     if ((unsigned)page_of >= (unsigned)a.pb.n_pages) {
-      atomicExch(a.status, ST_INVALID_ARG);
+      paged_bad_entry(a.status, a.pb);
       page_of = a.pb.n_pages;                                                     // (past the planes: the copy fills in zeros)
     }
   };
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(FW * 32, 2) k_paged_few(const PagedAttn a, con
   // (cluster) each block takes a part of the channels
   if (csize > 1) cluster_sync_all();
   else __syncthreads();
-  const bool skip = status_set(a.status) || *reinterpret_cast<volatile int*>(&abort_flag);   // (no partial result of a call that has failed)
+  const bool skip = paged_stopped(a.status, a.pb) || *reinterpret_cast<volatile int*>(&abort_flag);   // (no partial result of a call that has failed)
   for (int i = rank * (FW * 32) + threadIdx.x; i < rows * (DH / 4); i += csize * (FW * 32)) {
     const int rr = i / (DH / 4), c = (i % (DH / 4)) * 4;
     float M = s_M[rr], sum = s_L[rr];
@@ -349,12 +349,12 @@ __global__ void __launch_bounds__(NW * 32) k_paged_f32(const PagedAttn a) {
   pdl_wait();
   // (the word is read by one thread: other blocks of the call may raise it at any time, and a block whose threads had read different
   // values would go on with some of them, into barriers and shuffles of all)
-  if (tid == 0) s_skip = status_set(a.status);
+  if (tid == 0) s_skip = paged_stopped(a.status, a.pb);
   __syncthreads();
   PagedRequest r;
   int tile;
   if (!paged_unit<RT>(a, blockIdx.x, r, tile)) {
-    if (tid == 0) atomicExch(a.status, ST_INVALID_ARG);
+    if (tid == 0) paged_raise(a.status, a.pb);
     return;
   }
   if (r.b < 0 || s_skip) return;
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(NW * 32) k_paged_f32(const PagedAttn a) {
     fetch(kt + 1, a.v_plane, V);
   }
   cp_async_wait<0>();
-  if (bad_page) atomicExch(a.status, ST_INVALID_ARG);
+  if (bad_page) paged_bad_entry(a.status, a.pb);
 #pragma unroll
   for (int i = 0; i < RW; ++i) {
     if (wr + i >= rows) continue;          // (the whole warp)
@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(128) k_paged_merge(const PagedAttn a) {
   if (row >= rows) return;
   const int tok = (int)(row / a.hq);
   // (the lengths and the word say whether there is anything in the workspace; its entries are on their way meanwhile)
-  const bool mine = !status_set(a.status) && tok >= a.pb.cu[0] && tok < a.pb.cu[a.pb.batch];
+  const bool mine = !paged_stopped(a.status, a.pb) && tok >= a.pb.cu[0] && tok < a.pb.cu[a.pb.batch];
   float4 ml = lane < a.ranges ? a.part_ml[(size_t)lane * rows + row] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
   const float* p = a.part_o + (size_t)row * DH + c;
   float x[4][C];
@@ -757,7 +757,11 @@ phyai_status_t phyai_paged_attention(const phyai_paged_cache_t* cache, uint32_t 
   a.ranges = p.ranges, a.status = status_word, a.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
   a.part_ml = reinterpret_cast<float4*>(workspace), a.part_o = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(a.part_ml + (size_t)p.ranges * tokens * n_q_heads) + 31) & ~(uintptr_t)31);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  cudaError_t e = cudaErrorInvalidValue;
+  cudaError_t e = paged_call(status_word, &a.pb);
+  if (e != cudaSuccess) {
+    snprintf(g_paged_err, sizeof(g_paged_err), "status notes: %s", cudaGetErrorString(e));
+    return PHYAI_ERR_CUDA;
+  }
   if (p.f32) {
 #define PHYAI_F32_ROWS(DH) (p.rt == 4 ? launch_f32<DH, 2, 2>(a, p, st) : p.rt == 8 ? launch_f32<DH, 2, 4>(a, p, st) : p.rt == 16 ? launch_f32<DH, 2, 8>(a, p, st) : launch_f32<DH, 8, 8>(a, p, st))
     e = dh == 64 ? PHYAI_F32_ROWS(64) : dh == 128 ? PHYAI_F32_ROWS(128) : PHYAI_F32_ROWS(256);

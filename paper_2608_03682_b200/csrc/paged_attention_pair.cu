@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
 
   // ---- units of each request (both CTAs of a pair read the same lengths and come to the same list)
   pdl_wait();
-  if (tid == 0) s_skip = status_set(a.status), s_first[0] = 0;
+  if (tid == 0) s_skip = paged_stopped(a.status, a.pb), s_first[0] = 0;
   bool bad = false;
   for (int i = tid; i < a.pb.batch; i += PP_THREADS) {
     const int lo = a.pb.cu[i], hi = a.pb.cu[i + 1], kv = a.pb.kv_lens[i];
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     s_first[i + 1] = b ? 0 : (hi - lo + 2 * TOK - 1) / (2 * TOK);
   }
   bad = __syncthreads_or(bad);
-  if (bad && tid == 0) atomicExch(a.status, ST_INVALID_ARG);
+  if (bad && tid == 0) paged_raise(a.status, a.pb);
   const bool skip = s_skip != 0;
 
   // ---- what warp 2 goes by (and, once it has published its last unit, others): s_first: units (of one kv head) before each request; units of one kv
@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) __cluster_dims__(2, 1, 1)
     if (key >= r.kv) return past;
     const int page = a.pb.table[(size_t)r.b * a.pb.max_pages + (key >> a.pb.page_shift)];
     if ((unsigned)page >= (unsigned)a.pb.n_pages) {
-      atomicExch(a.status, ST_INVALID_ARG);
+      paged_bad_entry(a.status, a.pb);
       return past;
     }
     return (page << a.pb.page_shift) + (key & ((1 << a.pb.page_shift) - 1));

@@ -70,6 +70,118 @@ def test_rows_of_positions_outside_the_table_are_nan_and_no_others(src, dst, T, 
         check_heads(yk[good], k[good], None, table, positions[good], dst)
 
 
+def same(a, b):
+    return torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def some_bad(p, share=0.1):
+    """The table with an entry of some requests that names no page; their numbers."""
+    table, bad = p.table.copy(), []
+    for b, n in enumerate(p.kv_lens):
+        pages = -(-n // p.page)
+        if pages and p.rng.random() < share or not bad and b + 1 == len(p.kv_lens):
+            table[b, p.rng.integers(0, pages)] = p.rng.choice([-1, p.cache.n_pages, 2 ** 31 - 1, -2 ** 31])
+            bad.append(b)
+    return table, bad
+
+
+def rows_of(p, requests):
+    return np.concatenate([np.arange(p.cu[b], p.cu[b + 1]) for b in requests]).astype(np.int64)
+
+
+WAVES = [(8, 1, 256, [1] * 700, [20, 300] * 350, "bf16"), (16, 1, 64, [1] * 300, [40, 700, 90] * 100, "bf16"), (8, 2, 128, [1, 1, 2], [9001, 30, 3000], "bf16"),
+         (8, 1, 256, [2, 2], [3000, 2000], "bf16"), (8, 1, 256, [70, 150, 90] * 40, [70, 150, 300] * 40, "bf16"), (8, 2, 128, [40, 60, 1], [2500, 90, 700], "bf16"),
+         (4, 2, 128, [1] * 600, [48] * 600, "f32"), (8, 2, 128, [1, 2], [5000, 300], "f32"), (4, 1, 64, [30, 50], [300, 50], "f32")]
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens,dtype", WAVES)
+def test_attention_of_requests_beside_bad_entries(Hq, Hkv, dh, q_lens, kv_lens, dtype):
+    """In several waves of blocks, in key ranges, in units of pairs: their rows are what they are without, call after call; later calls write nothing."""
+    p = Paged(89, q_lens, kv_lens, Hkv, dh, 16, dtype, layers=1)
+    q, args = normal(p.rng, (p.T, Hq, dh), dtype).cuda(), p.device_args()
+    want = p.cache.attend(0, q, *args)
+    assert p.cache.poll_status() == 0
+    for _ in range(10):
+        table, bad = some_bad(p)
+        good = rows_of(p, np.setdiff1d(np.arange(len(q_lens)), bad))
+        out = torch.full_like(q, 5.0)
+        p.cache.attend(0, q, *args[:2], ints(table), out=out)
+        assert same(want[good], out[good])
+        out.fill_(5.0)
+        p.cache.attend(0, q, *args, out=out)
+        assert (out == 5.0).all() and p.cache.poll_status() == binding.ERR_INVALID_ARG
+    assert same(want, p.cache.attend(0, q, *args)) and p.cache.poll_status() == 0
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,src,dst,q_lens,kv_lens", [
+    (8, 1, 256, "bf16", "bf16", [1] * 700, [20, 300] * 350), (8, 2, 128, "f32", "bf16", [30, 90, 61] * 40, [30, 100, 200] * 40), (4, 1, 64, "f32", "f32", [17, 1], [17, 40])])
+def test_append_of_requests_beside_bad_entries(Hq, Hkv, dh, src, dst, q_lens, kv_lens):
+    p = Paged(90, q_lens, kv_lens, Hkv, dh, 16, dst, layers=1)
+    q, k, v = (normal(p.rng, (p.T, h, dh), src).cuda() for h in (Hq, Hkv, Hkv))
+    args, rope, before = p.device_args(), rope_table(400, dh).cuda(), p.cache.pages.clone()
+    want = p.cache.append(0, k, v, *args, rope, q=q)
+    after = p.cache.pages.clone()
+    for _ in range(10):
+        table, bad = some_bad(p)
+        keep = np.setdiff1d(np.arange(len(q_lens)), bad)
+        written = np.concatenate([P.slots(p.table[b], 16, kv_lens[b])[kv_lens[b] - q_lens[b]:] for b in keep])
+        theirs = np.concatenate([P.slots(p.table[b], 16, kv_lens[b])[kv_lens[b] - q_lens[b]:] for b in bad])
+        rest = np.setdiff1d(np.arange(before.shape[2]), np.concatenate([written, theirs]))
+        p.cache.pages.copy_(before)
+        got = p.cache.append(0, k, v, *args[:2], ints(table), rope, q=q)
+        st = p.cache.status.item()                                      # (0: the bad entry is of a page without new tokens)
+        assert st in (binding.OK, binding.ERR_INVALID_ARG)
+        good = rows_of(p, keep)
+        assert same(got[good], want[good]) and same(p.cache.pages[:, :, written].contiguous(), after[:, :, written].contiguous())
+        assert same(p.cache.pages[:, :, rest].contiguous(), before[:, :, rest].contiguous())
+        if st:
+            now = p.cache.pages.clone()
+            p.cache.append(0, v, k, *args, rope)
+            assert same(now, p.cache.pages) and p.cache.poll_status() == st
+
+
+@pytest.mark.parametrize("Hkv,dh,dtype,lens", [(1, 256, "bf16", [300, 20, 700] * 40), (2, 64, "f32", [40] * 300), (1, 64, "bf16", [40, 50])])
+def test_pack_of_requests_beside_bad_entries(Hkv, dh, dtype, lens):
+    p = Paged(91, [0] * len(lens), lens, Hkv, dh, 16, dtype, layers=3)
+    kv, total = ints(lens), sum(lens)
+    want, cu = p.cache.pack(ints(p.table), kv, total)
+    assert p.cache.poll_status() == 0
+    for _ in range(10):
+        table, bad = some_bad(p)
+        got, cu2 = p.cache.pack(ints(table), kv, total)
+        assert torch.equal(cu, cu2)
+        for b in np.setdiff1d(np.arange(len(lens)), bad):
+            assert same(got[:, :, cu[b]:cu[b + 1]].contiguous(), want[:, :, cu[b]:cu[b + 1]].contiguous())
+        out = torch.full_like(got, 5.0)
+        p.cache.pack(ints(p.table), kv, total, out=out)                 # the word is up
+        assert (out == 5.0).all() and p.cache.poll_status() == binding.ERR_INVALID_ARG
+
+
+def test_words_raised_by_entries_and_captured_calls():
+    """A replay goes by the word as any call does: raised by lengths or by another call it stops it, whatever the replay before met."""
+    p = Paged(92, [1, 1], [60, 40], 1, 64, 16)
+    q, (cu, lens, table) = normal(p.rng, (2, 4, 64)).cuda(), p.device_args()
+    out = p.cache.attend(1, q, cu, lens, table)
+    want, good = out.clone(), table.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.cache.attend(1, q, cu, lens, table, out=out)
+    table[1, 0] = -1
+    graph.replay()
+    assert torch.equal(out[0], want[0]) and p.cache.poll_status() == binding.ERR_INVALID_ARG
+    table.copy_(good)
+    for spoil in (lambda: p.cache.attend(1, q, cu, ints([60, -1]), table), lambda: p.cache.attend(1, q, cu, lens, torch.full_like(table, -1)),
+                  lambda: p.cache.status.fill_(binding.ERR_TIMEOUT),
+                  lambda: binding.norm_rope_heads(None, q, ints([0, 9]), rope_table(5, 64).cuda(), status=p.cache.status)):
+        spoil()
+        out.fill_(5.0)
+        graph.replay()
+        assert (out == 5.0).all() and p.cache.poll_status() != 0
+        graph.replay()
+        assert torch.equal(out, want) and p.cache.poll_status() == 0
+
+
 @pytest.mark.parametrize("lens,room", [([40, -1], 90), ([40, 16 * 5], 200), ([40, 50], 89), ([2 ** 31 - 1, 50], 90), ([-2 ** 31, 50], 90)])
 def test_pack_with_lengths_out_of_order_writes_nothing(lens, room):
     p = Paged(86, [0, 0], [40, 50], 1, 64, 16)                          # (a table of four pages and one entry more)
@@ -103,10 +215,6 @@ def test_poll_status_waits_for_calls_on_other_streams():
 # ------------------------------------------------------------------------------------------------------------------
 # waits that run out (the data that they wait for does arrive: nothing hangs)
 # ------------------------------------------------------------------------------------------------------------------
-def same(a, b):
-    return torch.equal(a.view(torch.uint8), b.view(torch.uint8))
-
-
 def expired(p, q, args, want, sure=True):
     """``sure``: a wait does expire (with a tile or two for each warp all copies may have come by the second poll: the call is good then)."""
     out = torch.full_like(q, 5.0)
