@@ -307,3 +307,66 @@ def test_every_row_that_sees_nan_or_infinite_logits_is_nan(value, Hq, Hkv, dh, q
     assert p.cache.poll_status() == 0
     sees = np.arange(int(p.cu[b + 1]) - (q_lens[b] + 1) // 2, int(p.cu[b + 1]))
     assert torch.isnan(got[sees]).all() and torch.isfinite(got[np.setdiff1d(np.arange(p.T), sees)]).all()
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# the kernels' forms for many units, many rows and long ranges, on picked rows
+# ------------------------------------------------------------------------------------------------------------------
+def run_picked(p, Hq, mask, every):
+    """Against the oracle on every ``every``-th token of a request, and its first and last: each as a request of one token over the keys that it sees."""
+    prefix = [n * 2 // 3 for n in p.kv_lens] if mask == "prefix" else None
+    q, args = normal(p.rng, (p.T, Hq, p.dh), p.dtype).cuda(), p.device_args()
+    out = torch.full_like(q, 777.0)
+    p.cache.attend(1, q, *args, causal=mask != "full", prefix_lens=None if prefix is None else ints(prefix), out=out)
+    assert p.cache.poll_status() == 0
+    live = np.arange(int(p.cu[0]), int(p.cu[-1]))
+    assert (out[np.setdiff1d(np.arange(p.T), live)] == 777.0).all()
+    tokens, seen, table = [], [], []
+    for b, (n, kv) in enumerate(zip(p.q_lens, p.kv_lens)):
+        lim = P.limits(n, kv, mask != "full", 0 if prefix is None else prefix[b])
+        for i in sorted((set(range(b % every, n, every)) | {0, n - 1}) & set(range(n))):
+            tokens.append(int(p.cu[b]) + i), seen.append(int(lim[i])), table.append(p.table[b])
+    planes = f64(p.cache.pages[1])
+    ref = P.attend(f64(q[tokens]), planes[0], planes[1], np.arange(len(tokens) + 1), seen, table, p.page, False)
+    check_attention(f64(out)[tokens], ref, p.dtype, p.dh, max(p.kv_lens))
+
+
+@pytest.mark.parametrize("mask", ["causal", "full", "prefix"])
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,past,page", [
+    (8, 1, 256, [968, 900, 701, 611, 968, 33, 850, 777], 0, 64),        # 187 units of 32 tokens: three rounds of 74 pairs
+    (8, 1, 256, [1500, 40, 1, 900], 333, 16),
+    (8, 2, 128, [700, 650, 512, 801, 90, 700, 333, 700], 0, 32),        # 146 units of 64 tokens and a kv head
+    (32, 8, 128, [300, 411, 65], 200, 128),
+    (16, 1, 64, [400, 390, 411, 17, 400, 512, 300, 399], 50, 256),      # 179 units of 16 tokens
+])
+def test_attention_of_more_units_than_pairs(Hq, Hkv, dh, q_lens, past, page, mask):
+    p = Paged(93, q_lens, [n + past * (i % 3) for i, n in enumerate(q_lens)], Hkv, dh, page, first_row=3, last_rows=2)
+    run_picked(p, Hq, mask, 29)
+
+
+@pytest.mark.parametrize("mask", ["causal", "full", "prefix"])
+@pytest.mark.parametrize("Hq,Hkv,dh", [(8, 8, 64), (12, 4, 64), (8, 8, 128), (8, 8, 256), (16, 2, 256)])
+def test_attention_fp32_of_many_rows(Hq, Hkv, dh, mask):
+    """Tiles of 64 rows: as many of them as there are SMs."""
+    q_lens = [700, 1, 0, 556]
+    assert sum(q_lens) * (Hq // Hkv) // 64 * Hkv >= 148
+    run_picked(Paged(94, q_lens, [900, 300, 5, 556], Hkv, dh, 32, "f32", first_row=1, last_rows=1), Hq, mask, 23)
+
+
+@pytest.mark.parametrize("mask", ["causal", "full", "prefix"])
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens", [
+    (8, 1, 256, [2], [9000]), (8, 1, 256, [2, 1], [5000, 7777]), (16, 1, 128, [1], [6001]), (8, 1, 64, [2, 2, 1], [8192, 17, 5000]),     # clusters of eight, ranges
+    (8, 2, 128, [4, 3], [5003, 9000]), (8, 1, 256, [2] * 20, [1100 + 37 * i for i in range(20)]), (16, 1, 64, [1] * 12, [4096] * 12),    # of eight, of one range
+    (8, 1, 256, [2] * 50, [700 + i for i in range(50)]), (16, 2, 128, [2] * 60, [600] * 60), (8, 1, 64, [2, 1] * 160, [300, 290] * 160),   # of four, two, one
+])
+def test_attention_of_nine_to_sixteen_rows(Hq, Hkv, dh, q_lens, kv_lens, mask):
+    run_picked(Paged(95, q_lens, kv_lens, Hkv, dh, 64, first_row=1, last_rows=2), Hq, mask, 1)
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,q_lens,kv_lens,dtype", [
+    (8, 1, 256, [1] * 64, [32768] + [600 + 5 * i for i in range(63)], "bf16"), (8, 2, 128, [1] * 63 + [65], [900] * 63 + [2000], "bf16"),
+    (8, 1, 256, [1] * 30 + [300], [700] * 30 + [900], "bf16"), (4, 1, 128, [1] * 20 + [100], [300] * 20 + [400], "f32"),
+])
+def test_attention_of_requests_of_very_different_lengths(Hq, Hkv, dh, q_lens, kv_lens, dtype):
+    """One long history among short ones; a chunk among single tokens."""
+    run_picked(Paged(96, q_lens, kv_lens, Hkv, dh, 64, dtype), Hq, "causal", 13)
