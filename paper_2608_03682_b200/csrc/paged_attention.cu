@@ -347,17 +347,16 @@ __global__ void __launch_bounds__(NW * 32) k_paged_f32(const PagedAttn a) {
   const int hk = blockIdx.y;
   pdl_launch_dependents();
   pdl_wait();
-  // (the word is read by one thread: other blocks of the call may raise it at any time, and a block whose threads had read different
-  // values would go on with some of them, into barriers and shuffles of all)
-  if (tid == 0) s_skip = paged_stopped(a.status, a.pb);
-  __syncthreads();
+  // (the word is read by one thread: it may go up at any time, and a block whose threads had read different values would go on with some of
+  // them, into barriers and shuffles of all.  On its way beside the lengths; looked at behind the first barrier.)
+  const int word = tid == 0 ? *reinterpret_cast<const volatile int*>(a.status) : ST_OK;
   PagedRequest r;
   int tile;
   if (!paged_unit<RT>(a, blockIdx.x, r, tile)) {
     if (tid == 0) paged_raise(a.status, a.pb);
     return;
   }
-  if (r.b < 0 || s_skip) return;
+  if (r.b < 0) return;
   const int rows = min(RT, r.n * a.group - tile * RT), row0 = tile * RT;
   const int n_keys = r.limit((row0 + rows - 1) / a.group, a.causal);
   const int tiles = (n_keys + XK - 1) / XK, ranges = ranges_of(tiles, a.ranges, 1), range = blockIdx.z;
@@ -387,7 +386,9 @@ __global__ void __launch_bounds__(NW * 32) k_paged_f32(const PagedAttn a) {
     cp_async_commit();
   };
   look_up(t0);
+  if (tid == 0) s_skip = word != ST_OK && paged_stopped(a.status, a.pb);
   __syncthreads();
+  if (s_skip) return;
   fetch(t0, a.k_plane, K);
   fetch(t0, a.v_plane, V);
   for (int i = tid; i < RT * (DH / 4); i += XT) {
