@@ -513,7 +513,7 @@ phyai_status_t phyai_batcher_plan(const phyai_batcher_config_t *cfg, uint32_t n,
  *   kv_lens     device int32 [batch]: cached tokens of request b WITH its new ones, which are the last; <= max_pages * page_size
  *   page_table  device int32 [batch][max_pages]: cached token t of request b is row page_table[b][t / page_size] * page_size +
  *               t % page_size of the planes; entries past a request's last page are not read
- *   batch <= 1024.  Requests may share pages that they only read; a page that two requests of an append write holds the tokens of
+ *   batch <= 1024, max_pages * page_size <= 2^31 - 256.  Requests may share pages that they only read; a page that two requests of an append write holds the tokens of
  *   either.
  *   status_word device int32, zeroed by the caller; a violation found on the device sets it to PHYAI_ERR_INVALID_ARG.
  *               Lengths out of order: the call writes nothing.  A table entry that names no page, a position outside the rotary table: nothing

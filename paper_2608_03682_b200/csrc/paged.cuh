@@ -13,6 +13,7 @@
 namespace phyai {
 
 constexpr int PAGED_MAX_BATCH = 1024;
+constexpr uint64_t PAGED_MAX_KEYS = 0x7fffff00ull;      // of a request: the kernels round a length up to tiles of keys, in 32 bits
 
 struct PagedBatch {
   const int* cu;          // [batch + 1]

@@ -708,7 +708,7 @@ size_t phyai_paged_attention_workspace_bytes(const phyai_paged_cache_t* cache, u
   const int n_sm = paged_sm_count();
   // (0 for calls that phyai_paged_attention refuses)
   if (!cache || !cache->n_kv_heads || !n_q_heads || n_q_heads % cache->n_kv_heads || !tokens || !batch || batch > (uint32_t)PAGED_MAX_BATCH || n_sm <= 0) return 0;
-  if ((uint64_t)tokens * (n_q_heads / cache->n_kv_heads) > 0x7fffffffull || (uint64_t)max_pages * cache->page_size > 0x7fffffffull) return 0;
+  if ((uint64_t)tokens * (n_q_heads / cache->n_kv_heads) > 0x7fffffffull || (uint64_t)max_pages * cache->page_size > PAGED_MAX_KEYS) return 0;
   return partial_bytes(make_plan(cache, (int)n_q_heads, (int)tokens, (int)batch, (int)max_pages, n_sm), (int)n_q_heads, (int)cache->head_dim, (int)tokens);
 }
 

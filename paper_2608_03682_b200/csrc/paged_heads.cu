@@ -419,7 +419,7 @@ phyai_status_t check_paged(const phyai_paged_cache_t* c, uint32_t layer, uint32_
   if (!batch || batch > (uint32_t)PAGED_MAX_BATCH) return bad_arg("batch must be 1..1024");
   if ((!all_layers && !cu) || !kv_lens || !table || !max_pages) return bad_arg("cu_q_lens, kv_lens or page_table is NULL, or max_pages is 0");
   if (!aligned4(cu) || !aligned4(kv_lens) || !aligned4(table)) return bad_arg("cu_q_lens, kv_lens and page_table must be 4-byte aligned");
-  if (tokens > 0x7fffffffu || (uint64_t)max_pages * c->page_size > 0x7fffffffull) return bad_arg("tokens or max_pages too large");
+  if (tokens > 0x7fffffffu || (uint64_t)max_pages * c->page_size > PAGED_MAX_KEYS) return bad_arg("tokens or max_pages too large");
   out->cu = cu, out->kv_lens = kv_lens, out->table = table, out->batch = (int)batch, out->tokens = (int)tokens, out->max_pages = (int)max_pages;
   out->page_shift = __builtin_ctz(c->page_size), out->n_pages = (int)c->n_pages;
   return PHYAI_OK;

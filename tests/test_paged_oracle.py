@@ -170,3 +170,14 @@ def test_packing_into_the_pages_is_refused(lib, dtype, bytes_of_a_row):
         lib.phyai_pack_paged_kv(None, 0, None, None, 0, None, 0, None, None, None)
         assert lib.phyai_pack_paged_kv(C.byref(c), 1, ADDRESS, ADDRESS, 2, at, 8, ADDRESS, ADDRESS, None) == BAD
         assert b"overlaps" in lib.phyai_paged_last_error()
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_tables_for_more_keys_than_the_kernels_count(lib, page):
+    """Lengths are rounded up to tiles of 128 keys in 32 bits."""
+    most = ((1 << 31) - 1) // page
+    while most * page > (1 << 31) - 256:
+        assert _attend(lib, _cache(page_size=page), most=most) == BAD
+        assert lib.phyai_paged_attention_workspace_bytes(C.byref(_cache(page_size=page)), 4, 2, 1, most) == 0
+        assert lib.phyai_pack_paged_kv(C.byref(_cache(page_size=page)), 1, ADDRESS, ADDRESS, most, 2 * ADDRESS, 8, ADDRESS, ADDRESS, None) == BAD
+        most -= 1
