@@ -1,5 +1,9 @@
 """The operators around a paged cache where calls go wrong or run long: bad entries and words that are up, waits that run out, other streams,
 and the kernels' forms for many units, many rows and long ranges, against the float64 oracle.  Tolerances: see test_gpu_paged.py."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -370,3 +374,31 @@ def test_attention_of_nine_to_sixteen_rows(Hq, Hkv, dh, q_lens, kv_lens, mask):
 def test_attention_of_requests_of_very_different_lengths(Hq, Hkv, dh, q_lens, kv_lens, dtype):
     """One long history among short ones; a chunk among single tokens."""
     run_picked(Paged(96, q_lens, kv_lens, Hkv, dh, 64, dtype), Hq, "causal", 13)
+
+
+# ------------------------------------------------------------------------------------------------------------------
+# captured calls
+# ------------------------------------------------------------------------------------------------------------------
+FIRST = """
+import sys, torch
+from paper_2608_03682_b200 import binding
+ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+pages, k, q = (torch.ones(s, device="cuda").bfloat16() for s in ((1, 2, 64, 1, 64), (4, 1, 64), (4, 4, 64)))
+cu, lens, table, pos, status, cache = ints([0, 4]), ints([20]), ints([[0, 1]]), ints([0, 1, 2, 3]), ints([0]), binding.PagedCache(pages, 16)
+rope = torch.zeros(10, 32, 2, device="cuda")
+calls = dict(heads=lambda: binding.norm_rope_heads(q, k, pos, rope, status=status)[1], append=lambda: cache.append(0, k, k, cu, lens, table, None, q=q),
+             attend=lambda: cache.attend(0, q, cu, lens, table), pack=lambda: cache.pack(table, lens, 20)[0])
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = calls[sys.argv[1]]()
+graph.replay()
+assert cache.poll_status() == 0 and int(status) == 0 and bool((out == (sys.argv[1] != "heads")).all())
+"""
+
+
+@pytest.mark.parametrize("call", ["heads", "append", "attend", "pack"])
+def test_the_first_call_of_a_process_may_be_captured(call):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST, call], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
