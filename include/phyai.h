@@ -561,6 +561,7 @@ phyai_status_t phyai_norm_rope_heads(const phyai_heads_desc_t *desc, uint32_t to
  * Append: K (normed and rotated as above) and V of the new tokens go to their places in the pages of `layer`; with q, its normed and
  * rotated rows go to q_out in the same pass.  kv_lens counts the new tokens already: cu[b + 1] - cu[b] <= kv_lens[b].
  *   positions   device int32 [tokens] for the rotation, or NULL: the token's place in its cache
+ *   q_out       as above; q, k and v overlap no page rows that the call writes
  *   desc        n_kv_heads, head_dim, out_dtype as the cache's
  */
 phyai_status_t phyai_append_paged_kv(const phyai_paged_cache_t *cache, const phyai_heads_desc_t *desc, uint32_t layer, uint32_t tokens,
@@ -570,7 +571,8 @@ phyai_status_t phyai_append_paged_kv(const phyai_paged_cache_t *cache, const phy
                                      const float *q_gain, const float *k_gain, void *q_out, int32_t *status_word, void *stream);
 
 /*
- * Attention of the new tokens over the pages of `layer` (their own keys and values have been appended).  Row i of request b, at place
+ * Attention of the new tokens over the pages of `layer` (their own keys and values have been appended).  fp32 statistics and sums; a BF16 cache's softmax
+ * weights are rounded to bf16 ahead of their product with V (each by 2^-8 of itself at most; their sum is of the unrounded ones).  Row i of request b, at place
  * p = kv_lens[b] - (cu[b + 1] - cu[b]) + i of its cache, sees keys [0, limit):
  *   causal 0    limit = kv_lens[b]
  *   causal 1    limit = max(p + 1, prefix_lens[b]), at most kv_lens[b]; prefix_lens: device int32 [batch] or NULL (0): image and prompt

@@ -588,7 +588,8 @@ def norm_rope_heads(q: Optional[torch.Tensor], k: torch.Tensor, positions: Optio
                     dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None, stream=None):
     """Norm (gain ``1 + gain``; None: no norm) of every head of ``q`` ``[T, Hq, dh]`` and ``k`` ``[T, Hkv, dh]`` with the rotation by
     ``positions`` (int32 ``[T]``) in the same pass; rows may be columns of a fused matrix.  Returns (q, k) in ``dtype`` (default: as
-    given).  The rows of a token whose position is outside the table are NaN; ``status``: int32 word that it raises as well (zeroed by the caller)."""
+    given).  The rows of a token whose position is outside the table are NaN; ``status``: int32 word that it raises as well (zeroed by the caller).
+    Results carry no gradients."""
     lib = _lib or load_library()
     device, src = k.device, k.dtype
     index = device.index
@@ -638,7 +639,7 @@ class PagedCache:
     A call's requests: ``cu_q_lens`` int32 ``[B + 1]`` (rows of the new tokens), ``kv_lens`` int32 ``[B]`` (cached tokens with the new
     ones), ``page_table`` int32 ``[B, max_pages]``; see ``phyai.h``.  What a call finds wrong on the device raises the cache's status word
     (``poll_status``), and later calls write nothing until it has been read; a table entry that names no page leaves the call's other requests
-    as they would be.  Streams: calls on the cache are ordered by the caller."""
+    as they would be.  Streams: calls on the cache are ordered by the caller.  Serving only: results carry no gradients."""
 
     def __init__(self, pages: torch.Tensor, page_size: int):
         self.lib = load_library()

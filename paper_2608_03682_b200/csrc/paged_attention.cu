@@ -13,8 +13,11 @@
 //   O^T += V^T P^T   V^T by transposing ldmatrix
 // The warps of a block merge through shared memory, the blocks of a cluster through distributed shared memory, several clusters of a
 // row (key ranges) through a second kernel.
-// Measured, one token a request: 8 heads of 256, 64 requests of 601 - 969 keys 12.5 us, 4.1 TB/s, 256 41 us, 5.0 TB/s, one request of 969 keys 8.2 us (start, lengths ->
-// pages -> copies, cluster merge: a chain of trips to the L2); 8 heads of 128 over 8 x 24576 - 32768 keys 47.0 us, 5.0 TB/s (5.9 between start and merge).
+// Measured, one token a request, keys and values from memory (other requests' calls between two of the same): 8 heads of 256, 64 requests of 601 - 969 keys
+// 16.5 us, 3.2 TB/s (12.7 where the 51 MB lie in the L2), 256 43 us, 4.8 TB/s, one request of 969 keys 9.3 us (8.4; start, lengths -> pages ->
+// copies, cluster merge: a chain of trips to the L2); 8 heads of 128 over 8 x 24576 - 32768 keys 50 us with the merge, 4.7 TB/s.  Figures of variants below: of one
+// state over and over, in the L2 as far as it fits.  What lengths cannot do: every row tile gets the same clusters, as the host does not know them; one
+// request of 32768 keys among 63 of 800 takes 113 us, four blocks' time, where 64 of 800 take 16.6.
 #include <atomic>
 #include <cstdio>
 #include <cstring>
@@ -332,9 +335,10 @@ constexpr int XK = 32;                   // keys per tile
 // are broadcasts (with 8 keys a load, repeated for 4 rows, shared memory bounded the kernel at a third of the rate); P V: a lane takes DH / 32
 // channels, P are the broadcasts.  The next tile's K is on its way while P V of this one is computed, its V under the next logits; a tile's
 // rows in the planes are looked up once, a tile ahead.
-// Measured: four requests of 17 tokens over 33 - 81 keys 8.4 us (the chain of a tile or two); one token over 8 x 8192 keys, 2 kv heads of 128,
-// 42 us, 3.2 TB/s; 64 requests of 600 - 968 keys, 8 heads of 256: 54 us, 1.9 TB/s (every pair of rows reads the tile from shared memory; a row a warp
-// 48 and 62, four rows a warp 42 and 57); chunks of 512 tokens 25 TFLOP/s, about a third of the FMA rate: eight warps an SM, in step through four barriers a tile.
+// Measured: four requests of 17 tokens over 33 - 81 keys 8.8 us, 10.6 - 12 from memory (the chain of a tile or two); one token over 8 x 8192 keys, 2 kv heads of 128,
+// 44 us, 3.0 TB/s; 64 requests of 600 - 968 keys, 8 heads of 256: 56 us, 1.8 TB/s (every pair of rows reads the tile from shared memory; a row a warp
+// 48 and 62, four rows a warp 42 and 57, for 42 and 54 then); four chunks of 512 tokens over 2048 keys 20 TFLOP/s, a quarter of the FMA rate: eight warps an SM,
+// in step through four barriers a tile.
 template <int DH, int RW, int NW>
 __global__ void __launch_bounds__(NW * 32) k_paged_f32(const PagedAttn a) {
   constexpr int XT = NW * 32, RT = NW * RW, PITCH = DH + 4, PP = XK + 4, C = DH / 32, CV = C < 4 ? C : 4, CJ = C / CV, RB = RW < 4 ? RW : 4;
@@ -604,7 +608,9 @@ Plan make_plan(const phyai_paged_cache_t* c, int hq, int tokens, int batch, int 
   const long long rows = (long long)tokens * group;
   p.f32 = c->dtype == PHYAI_F32;
   const long long keys = (long long)max_pages * c->page_size;
-  // More than 16 packed rows a request: the tensor cores' kernel, whose tiles of 256 rows cost what a tile's keys cost to fetch.
+  // More than 16 packed rows a request: the tensor cores' kernel, whose tiles of 256 rows cost what a tile's keys cost to fetch.  The average is
+  // all that the host knows, and a chunk beside single tokens is not the average: 63 single tokens over 1000 keys with a chunk of 65, 8 heads of 256,
+  // 36 us here, with one of 66 (the other kernel) 25; the chunk over 16000 keys 117 and 83.  21 single tokens over 700 keys: 16.7 and 18.1.
   if (!p.f32 && rows > 16ll * holders && paged_pair_supported((int)c->head_dim, group)) {
     const int per = paged_pair_tokens(group), pairs = paged_pair_resident((int)c->head_dim);
     const long long full = (tokens + per - 1) / per > holders ? (tokens + per - 1) / per : holders;

@@ -20,8 +20,8 @@
 // Warps of a CTA: 0 fetches K and Q, 1 V; 2 goes through the units; 3 issues the MMAs (leader CTA); 4-19 softmax, correction, output.  Every
 // wait is bounded; after a give-up the protocol runs to its end and only the global stores are skipped.
 //
-// Measured: eight prefixes of 968 tokens (8 heads of 256, one kv head) 68 us, 0.9 PFLOP/s (SM clock about 1.6 GHz, the power cap); four chunks of 384 -
-// 512 tokens over 4096 - 8192 keys (8 heads of 128, two kv heads) 62.6 us with the merge, 0.7 PFLOP/s; eight prefixes with 16 heads of 64 74 us.
+// Measured, all operands from memory: eight prefixes of 968 tokens (8 heads of 256, one kv head) 69 - 71 us, 0.9 PFLOP/s (SM clock about 1.6 GHz, the power cap); four chunks of
+// 384 - 512 tokens over 4096 - 8192 keys (8 heads of 128, two kv heads) 63.8 us with the merge, 0.7 PFLOP/s; eight prefixes with 16 heads of 64 75 us.
 // What bounds it, by clocks taken in the kernel: head_dim 256: a tile takes 2150 clocks, of which the products 2048; a unit's end 3700
 // to 5600, in which its output goes out and the next one's queries come in through the L2 on all SMs at a time (starting the pairs apart: 71 us
 // for 68); four rounds of units where 3.35 would do.  head_dim 128: a tile takes 2050, the products 1024 of it: the chain logits -> maximum (400) ->

@@ -10,8 +10,10 @@
 // channels are pairs, a warp's next to one another: a pair's table entry is 16 bytes, so that a load of the table or the gains takes as few passes of
 // the L1 as it can (with 8 channels in a row, one load of 16 bytes, a lane's entries are 64 bytes apart: 17.1 for 15.0 us).  The arithmetic is
 // fp32 with one rounding at the store.
-// Measured: 7744 tokens of 9 heads of 256 (pi0), bf16: 15.0 us, 4.8 TB/s; with the append (k, v into pages) 14.5.  64 tokens: 2 - 3 us, the
-// chain lengths -> page -> table -> store.  Packing 258 MB: 38.9 us, 6.0 TB/s of 6.55 that a copy reaches.
+// Measured: 7744 tokens of 9 heads of 256 (pi0), bf16, rows from memory: 16.5 us, 4.4 TB/s (14.6 where the 72 MB lie in the L2, as in the figures of variants
+// here); 6272 tokens with the append (k, v into pages) 17.0 (14.5).  Nothing is full (58 % of the issue slots, 43 % of the L1): a warp loads two slots, computes,
+// stores and only then loads again.  64 tokens: 2 - 3 us, the chain lengths -> page -> table -> store.  Packing 231 MB: 39.2 us, 5.9 TB/s of 6.55
+// that a copy reaches.
 #include <atomic>
 #include <cstdio>
 
