@@ -657,9 +657,16 @@ class PagedCache:
         self._status_ptr = self.status.data_ptr()
         self._sizes: Dict[tuple, int] = {}     # sizes of a call -> bytes of its workspace
 
-    def poll_status(self) -> int:
-        """Read-and-clear the status word, once every call on the cache so far has run (waits for the device: calls may be on any stream, or
-        replayed from graphs); returns the status code."""
+    def poll_status(self, stream=None) -> int:
+        """Read-and-clear the status word, once every call on the cache so far has run; returns the status code.  Waits for the device, since calls may
+        be on any stream or replayed from graphs, or with ``stream`` for that one alone: the only one with such calls since the last poll."""
+        if stream is not None:
+            with _Elsewhere(self.device, stream):
+                st = int(self.status.item())
+                if st:
+                    self.status.zero_()
+                    stream.synchronize()
+            return st
         torch.cuda.synchronize(self.device)
         st = int(self.status.item())
         if st:

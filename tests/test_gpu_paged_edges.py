@@ -3,6 +3,7 @@ and the kernels' forms for many units, many rows and long ranges, against the fl
 import os
 import subprocess
 import sys
+import types
 
 import numpy as np
 import pytest
@@ -214,6 +215,25 @@ def test_poll_status_waits_for_calls_on_other_streams():
         assert p.cache.poll_status() == binding.ERR_INVALID_ARG
         got = p.cache.attend(1, q, *args, stream=side)                  # the word is down for any stream
         assert p.cache.poll_status() == 0 and torch.equal(want, got)
+
+
+def test_poll_status_of_one_stream_does_not_wait_for_others():
+    p = Paged(97, [1, 2], [50, 40], 1, 64, 16)
+    q, args = normal(p.rng, (p.T, 4, 64)).cuda(), p.device_args()
+    bad, side, other, done = torch.full_like(args[2], -1), torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.Event()
+    want = p.cache.attend(1, q, *args)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(other):
+        torch.cuda._sleep(1_000_000_000)                                # half a second
+        done.record()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    p.cache.attend(1, q, *args[:2], bad, stream=side)
+    assert p.cache.poll_status(side) == binding.ERR_INVALID_ARG and not done.query()
+    got = p.cache.attend(1, q, *args)                                   # the word is down for any stream
+    assert p.cache.poll_status() == 0 and done.query() and torch.equal(want, got)
+    with pytest.raises(ValueError):
+        p.cache.poll_status(types.SimpleNamespace(device=torch.device("cuda", 1)))
 
 
 # ------------------------------------------------------------------------------------------------------------------
