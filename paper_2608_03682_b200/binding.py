@@ -583,6 +583,18 @@ def _paged_fail(lib, st: int):
     raise PhyaiError(st, lib.phyai_paged_last_error().decode())
 
 
+_unread_words: Dict[int, torch.Tensor] = {}     # device index -> the status word of norm_rope_heads calls without one: written, never read
+
+
+def _unread_word(index: int, device: torch.device) -> torch.Tensor:
+    w = _unread_words.get(index)
+    if w is None:
+        w = torch.empty(1, dtype=_I32, device=device)
+        if not torch.cuda.is_current_stream_capturing():     # (not out of a graph's memory)
+            _unread_words[index] = w
+    return w
+
+
 def norm_rope_heads(q: Optional[torch.Tensor], k: torch.Tensor, positions: Optional[torch.Tensor], rope_cos_sin: Optional[torch.Tensor],
                     q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
                     dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None, stream=None):
@@ -618,7 +630,7 @@ def norm_rope_heads(q: Optional[torch.Tensor], k: torch.Tensor, positions: Optio
         q_out_ptr = q_out.data_ptr()
     k_out = _empty_rows(T, Hkv, dh, dtype, device)
     if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=device)
+        status = _unread_word(index, device)
     st = lib.phyai_norm_rope_heads(desc[1], T, q_ptr, q_row, k.data_ptr(), k_row, pos, rope, n_pos, gq, gk, q_out_ptr, k_out.data_ptr(),
                                    _ints("status", status, index, (1,)), _current_stream(index))
     if st != OK:

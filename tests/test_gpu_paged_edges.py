@@ -422,3 +422,23 @@ def test_the_first_call_of_a_process_may_be_captured(call):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST, call], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr
+
+
+def test_heads_without_a_word_in_a_graph_and_out_of_it():
+    """The first such call of a device in a capture, replayed, and calls out of it, with positions outside the table."""
+    binding._unread_words.clear()
+    rng = np.random.default_rng(98)
+    k, table = normal(rng, (40, 2, 64)).cuda(), rope_table(50, 64)
+    positions, rope = rng.integers(0, 50, 40), table.cuda()
+    positions[7] = 50
+    pos, good = ints(positions), np.setdiff1d(np.arange(40), [7])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        first, second = (binding.norm_rope_heads(None, k, pos, rope)[1] for _ in range(2))
+    for _ in range(3):
+        graph.replay()
+        third = binding.norm_rope_heads(None, k, pos, rope)[1]
+        for y in (first, second, third):
+            assert torch.isnan(y[7]).all()
+            check_heads(y[good], k[good], None, table, positions[good], "bf16")
